@@ -303,8 +303,119 @@ enum { ANAKIN_PROBE_MFMA_F32 = 0, ANAKIN_PROBE_MFMA_BF16 = 1, ANAKIN_PROBE_COPY 
 int32_t anakin_peak_probe(int32_t kind, int32_t workgroups, void* scratch, size_t scratch_bytes, void* hip_stream,
                           double* amount, double* milliseconds);
 
+/* ---- operators of token policies ----
+ * The losses and targets above are tied to a handle's own few head outputs.  These calls take them to any policy that
+ * picks one of `vocab` choices per row of a matrix of logits (a row being a token of a sequence, or a sample of an
+ * unroll): log-probabilities, a clipped policy loss, a loss over pairs of sequences, and returns over sequences of
+ * unequal length.  No handle: the caller passes device pointers, a workspace (256-byte aligned, of the size the
+ * matching *_workspace_bytes returns) and a stream of the device that holds them, which has to be the current device;
+ * everything is enqueued on that stream, nothing synchronises, and nothing is kept between calls.  Two calls that may
+ * overlap in time need workspaces of their own.  Calls can be captured into a HIP graph.  Errors are found on the host
+ * before anything is enqueued; anakin_last_error(NULL) has the message (per thread).  Results do not depend on
+ * scheduling: no floating-point atomics. */
+enum { ANAKIN_TYPE_FP32 = 0, ANAKIN_TYPE_BF16 = 1, ANAKIN_TYPE_FP16 = 2 };
+enum { ANAKIN_INDEX_U8 = 0, ANAKIN_INDEX_I32 = 1, ANAKIN_INDEX_I64 = 2 };
+
+/* A matrix of logits [rows][vocab] of `type`, `row_stride` elements from row to row (>= vocab; columns adjacent), and
+ * the column each row chose.  The policy is softmax(scale * logits): scale is one over the sampling temperature.
+ * rows < 2^31, vocab < 2^28.  A logit of minus infinity is a choice that is not allowed.
+ * A row whose target lies outside [0, vocab) takes no part: its logits are not read and may hold anything. */
+typedef struct {
+    const void* d_logits;
+    int64_t rows, vocab, row_stride;
+    const void* d_target;
+    int32_t type, target_type;        /* ANAKIN_TYPE_*, ANAKIN_INDEX_* */
+    double scale;
+} anakin_rows;
+
+/* Workspace of the calls that take an anakin_rows (pairs: of the preference loss, else 0).  0 for sizes out of range. */
+size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64_t pairs);
+
+/* logp[n] = log softmax(scale * logits[n])[target[n]], lse[n] = log sum exp(scale * logits[n]), and (where not null)
+ * entropy[n] = -sum p log p.  Rows that take no part get zeros; a row all of whose logits are minus infinity gets
+ * logp = lse = -inf and entropy 0. */
+int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy,
+                              void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its backward pass: dlogits[n][j] = scale (g[n] ([j = target[n]] - p_j) - e[n] p_j (log p_j + entropy[n])) with
+ * g = d_grad_logp, e = d_grad_entropy (null: 0; else d_entropy has to be given) and p from the lse of the forward call.
+ * dlogits has the logits' type, grad_stride elements from row to row; it may be the logits themselves (same pointer and
+ * stride), and else must not overlap them.  Rows that take no part get zeros. */
+int32_t anakin_token_logprobs_backward(const anakin_rows* x, const float* d_lse, const float* d_entropy,
+                                       const float* d_grad_logp, const float* d_grad_entropy,
+                                       void* d_dlogits, int64_t grad_stride, void* hip_stream);
+
+/* Clipped policy loss with a KL term and an entropy bonus, and its gradient, in one call.  With lp = log pi(target) and
+ * r = exp(lp - logp_old):  l = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - d - 1) - entropy_coef H,
+ * d = logp_ref - lp (the estimator of KL(pi || ref) that is never negative), and L = sum w l / W over the rows that take
+ * part, W = sum w, or `norm` where that is not 0 (a batch cut into several calls).  d_weight null: 1; a row of weight 0
+ * takes no part.  d_logp_ref may be null where kl_coef is 0.  W = 0 gives loss and gradient 0.
+ * d_dlogits (null: the loss alone) = grad_scale dL/dlogits, as in the backward pass above.  Rows that take no part get
+ * zero gradient and logp; a row of minus infinities counts with loss and gradient 0.
+ * d_stats[8]: L, and weighted means over W: policy term, e^d - d - 1 (0 without reference), entropy, share of clipped
+ * rows, ratio; then W and the number of rows that took part.  d_logp (may be null): lp. */
+typedef struct {
+    const float *d_logp_old, *d_adv, *d_logp_ref, *d_weight;
+    double clip_low, clip_high, kl_coef, entropy_coef, norm, grad_scale;
+    float *d_stats, *d_logp;
+    void* d_dlogits;
+    int64_t grad_stride;
+} anakin_policy_args;
+int32_t anakin_policy_loss(const anakin_rows* x, const anakin_policy_args* a, void* d_workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/* Sequences over rows.  PACKED: sequence s is rows d_offsets[s] .. d_offsets[s + 1] - 1 (count + 1 ascending values).
+ * BATCH: token j of s is row s * length + j; TIME: row j * count + s; of d_lengths[s] tokens each (null: length).
+ * Sequences of length 0 are allowed.  Offsets that descend or leave the rows, and lengths outside [0, length], are an
+ * error that only the device can see: they are cut to what exists, nothing else is read or written, and the call's
+ * results are then of no use (the preference loss says so with a loss of NaN). */
+enum { ANAKIN_LAYOUT_PACKED = 0, ANAKIN_LAYOUT_BATCH = 1, ANAKIN_LAYOUT_TIME = 2 };
+typedef struct {
+    int32_t layout;
+    int64_t count, length;
+    const int64_t* d_offsets;
+    const int32_t* d_lengths;
+} anakin_sequences;
+
+/* Loss over pairs of sequences from their summed log ratios, and its gradient.  The first count / 2 sequences are
+ * paired with the other half in order.  D_s = sum over the tokens of s that take part of lp - logp_ref (d_logp_ref
+ * null: lp), divided by their number where `mean` is set; h = beta (D_first - D_second) - margin;
+ * l = -y log sigmoid(h) - (1 - y) log sigmoid(-h) with y = d_label[pair] in [0, 1], how far the first of the pair is
+ * preferred (null: 1); L = sum w l / W over the pairs, W = sum w or `norm`; d_weight null: 1, a pair of weight 0 takes
+ * no part.  d_dlogits (null: the loss alone) = grad_scale dL/dlogits; rows in no pair get zeros.
+ * d_stats[8]: L, and weighted means of [h > 0], beta D_first, beta D_second, h; then W, the pairs and the tokens that
+ * took part.  d_margins (may be null) [count / 2]: h; d_logp (may be null): lp of every row with a target. */
+typedef struct {
+    const float *d_logp_ref, *d_label, *d_weight;
+    double beta, margin, norm, grad_scale;
+    int32_t mean;
+    float *d_stats, *d_margins, *d_logp;
+    void* d_dlogits;
+    int64_t grad_stride;
+} anakin_preference_args;
+int32_t anakin_preference_loss(const anakin_rows* x, const anakin_sequences* seq, const anakin_preference_args* a,
+                               void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* lambda-returns and advantages over sequences: G_t = r_t + disc_t ((1 - lambda) V_{t+1} + lambda G_{t+1}),
+ * adv_t = G_t - V_t, disc_t = gamma, 0 where done[t] != 0; behind the last token V = G = bootstrap[s] (null: 0).
+ * rewards fp32, values of value_type; d_adv / d_ret fp32, [rows] (neither may overlap an input).  Rows in no sequence
+ * get zeros. */
+typedef struct {
+    int64_t rows;
+    const float* d_reward;
+    const void* d_value;
+    const uint8_t* d_done;
+    const float* d_bootstrap;
+    int32_t value_type;
+    double gamma, lambda_;
+    float *d_adv, *d_ret;
+} anakin_returns_args;
+size_t anakin_returns_workspace_bytes(int64_t rows, int64_t count);
+int32_t anakin_lambda_returns(const anakin_sequences* seq, const anakin_returns_args* a, void* d_workspace,
+                              size_t workspace_bytes, void* hip_stream);
+
 /* Handle-owned message for the last error on this handle (valid until the next
- * call on it); for a null handle, the message of the last failed create. */
+ * call on it); for a null handle, the message of this thread's last failed create or operator call. */
 const char* anakin_last_error(const anakin_t* h);
 
 #ifdef __cplusplus

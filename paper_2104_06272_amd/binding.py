@@ -59,6 +59,32 @@ class Plan(C.Structure):
                 ("dx_rows", C.c_int32 * 4), ("bf16_matrix_path", C.c_int32), ("updates_per_unroll", C.c_int32)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64), ("target", C.c_void_p),
+                ("type", C.c_int32), ("target_type", C.c_int32), ("scale", C.c_double)]
+
+
+class PolicyArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("logp_old", "adv", "logp_ref", "weight")]
+                + [(n, C.c_double) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef", "norm", "grad_scale")]
+                + [(n, C.c_void_p) for n in ("stats", "logp", "dlogits")] + [("grad_stride", C.c_int64)])
+
+
+class SequenceArgs(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("count", C.c_int64), ("length", C.c_int64), ("offsets", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class PreferenceArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("logp_ref", "label", "weight")]
+                + [(n, C.c_double) for n in ("beta", "margin", "norm", "grad_scale")] + [("mean", C.c_int32)]
+                + [(n, C.c_void_p) for n in ("stats", "margins", "logp", "dlogits")] + [("grad_stride", C.c_int64)])
+
+
+class ReturnsArgs(C.Structure):
+    _fields_ = ([("rows", C.c_int64)] + [(n, C.c_void_p) for n in ("reward", "value", "done", "bootstrap")]
+                + [("value_type", C.c_int32), ("gamma", C.c_double), ("lambda_", C.c_double), ("adv", C.c_void_p), ("ret", C.c_void_p)])
+
+
 class KernelTime(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("calls", C.c_int64), ("total_ms", C.c_double)]
 
@@ -68,6 +94,8 @@ EXPORTS = ["anakin_workspace_bytes", "anakin_create", "anakin_rollout", "anakin_
            "anakin_get_opt_state", "anakin_set_opt_state", "anakin_get_env_state", "anakin_set_env_state",
            "anakin_get_walls", "anakin_get_global_step", "anakin_set_global_step", "anakin_get_trajectory",
            "anakin_get_metrics", "anakin_get_plan", "anakin_set_mode", "anakin_set_updates_per_unroll", "anakin_set_update_chunk_mode", "anakin_set_policy_gradient", "anakin_profile", "anakin_kernel_times", "anakin_peak_probe",
+           "anakin_rows_workspace_bytes", "anakin_token_logprobs", "anakin_token_logprobs_backward", "anakin_policy_loss", "anakin_preference_loss",
+           "anakin_returns_workspace_bytes", "anakin_lambda_returns",
            "anakin_last_error"]
 
 _lib = None
@@ -90,7 +118,6 @@ def load():
     L = C.CDLL(LIB_PATH)
     vp, f32p, i32p, u32p = C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32), C.POINTER(C.c_uint32)
     L.anakin_workspace_bytes.argtypes = [C.POINTER(EnvCfg), C.POINTER(NetCfg), C.c_int32, C.c_int32]
-    L.anakin_workspace_bytes.restype = C.c_size_t
     L.anakin_create.argtypes = [C.POINTER(vp), C.POINTER(EnvCfg), C.POINTER(NetCfg), C.c_int32, C.c_int32,
                                 C.c_uint64, vp, C.c_size_t, vp]
     for name in ("anakin_rollout", "anakin_learn", "anakin_step", "anakin_step_decoupled", "anakin_set_actor_stream", "anakin_destroy"):
@@ -119,8 +146,19 @@ def load():
     L.anakin_last_error.argtypes = [vp]
     L.anakin_last_error.restype = C.c_char_p
     L.anakin_peak_probe.argtypes = [C.c_int32, C.c_int32, vp, C.c_size_t, vp, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    i64, sz, rows, seq = C.c_int64, C.c_size_t, C.POINTER(Rows), C.POINTER(SequenceArgs)
+    L.anakin_rows_workspace_bytes.argtypes = [i64, i64, i64]
+    L.anakin_returns_workspace_bytes.argtypes = [i64, i64]
+    L.anakin_token_logprobs.argtypes = [rows, vp, vp, vp, vp, sz, vp]
+    L.anakin_token_logprobs_backward.argtypes = [rows, vp, vp, vp, vp, vp, i64, vp]
+    L.anakin_policy_loss.argtypes = [rows, C.POINTER(PolicyArgs), vp, sz, vp]
+    L.anakin_preference_loss.argtypes = [rows, seq, C.POINTER(PreferenceArgs), vp, sz, vp]
+    L.anakin_lambda_returns.argtypes = [seq, C.POINTER(ReturnsArgs), vp, sz, vp]
+    sizes = ("anakin_workspace_bytes", "anakin_rows_workspace_bytes", "anakin_returns_workspace_bytes")
+    for name in sizes:
+        getattr(L, name).restype = sz
     for name in EXPORTS:
-        if name not in ("anakin_workspace_bytes", "anakin_last_error"):
+        if name not in sizes + ("anakin_last_error",):
             getattr(L, name).restype = C.c_int32
     _lib = L
     return L

@@ -15,6 +15,7 @@
 using namespace ank;
 
 static thread_local std::string g_create_error;
+namespace ank { std::string& call_error() { return g_create_error; } }
 
 // ---- the library's own update scratch, for callers that cannot allocate (anakin_learn_static) --------------
 // One array per GPU (every device that loads the library holds its own copy until the process ends).  In host
