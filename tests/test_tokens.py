@@ -277,7 +277,7 @@ def _pref(**over):
 
 
 def _ret(**over):
-    a = dict(rows=8, reward=FAKE, value=FAKE, done=None, bootstrap=None, value_type=0, gamma=1.0, lambda_=0.9, adv=FAKE, ret=FAKE)
+    a = dict(rows=8, reward=FAKE, value=FAKE, done=None, bootstrap=None, value_type=0, gamma=1.0, lambda_=0.9, adv=FAKE + 0x100000, ret=FAKE + 0x200000)
     a.update(over)
     return binding.ReturnsArgs(*[a[k] for k, _ in binding.ReturnsArgs._fields_])
 
@@ -297,7 +297,8 @@ def test_pairs_and_returns_are_checked_on_the_host(lib):
     assert lib.anakin_preference_loss(_rows(), _seq(), _pref(), FAKE, 256, None) == binding.E_WORKSPACE_TOO_SMALL
     for over in (dict(beta=math.nan), dict(margin=math.inf), dict(norm=-1.0), dict(stats=None), dict(dlogits=FAKE + 0x200000, grad_stride=3)):
         assert lib.anakin_preference_loss(_rows(), _seq(), _pref(**over), FAKE, 1 << 30, None) == binding.E_INVALID_ARG, over
-    for over in (dict(gamma=1.5), dict(gamma=math.nan), dict(lambda_=-0.1), dict(value_type=4), dict(reward=None), dict(value=None), dict(adv=None), dict(ret=None), dict(rows=-1)):
+    for over in (dict(gamma=1.5), dict(gamma=math.nan), dict(lambda_=-0.1), dict(value_type=4), dict(reward=None), dict(value=None), dict(adv=None), dict(ret=None), dict(rows=-1),
+                 dict(adv=FAKE), dict(ret=FAKE + 28), dict(ret=FAKE + 0x100000), dict(done=FAKE + 0x100000), dict(bootstrap=FAKE + 0x200010)):
         assert lib.anakin_lambda_returns(_seq(), _ret(**over), FAKE, 1 << 30, None) == binding.E_INVALID_ARG, over
     assert lib.anakin_lambda_returns(_seq(), None, FAKE, 1 << 30, None) == binding.E_INVALID_ARG
     assert lib.anakin_lambda_returns(_seq(), _ret(), FAKE, 0, None) == binding.E_WORKSPACE_TOO_SMALL
