@@ -328,7 +328,8 @@ typedef struct {
     double scale;
 } anakin_rows;
 
-/* Workspace of the calls that take an anakin_rows (pairs: of the preference loss, else 0).  0 for sizes out of range. */
+/* Workspace of the calls that take an anakin_rows; pairs: count / 2 for the preference loss, 1 at least, and 0 for the
+ * other calls.  Returns 0 for sizes out of range. */
 size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64_t pairs);
 
 /* logp[n] = log softmax(scale * logits[n])[target[n]], lse[n] = log sum exp(scale * logits[n]), and (where not null)

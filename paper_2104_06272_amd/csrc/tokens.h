@@ -16,7 +16,8 @@ struct Rows {
     int64_t rows, stride;
     int V, target_type;
     float c;
-    double scale, dc;                            // dc: the exact product minus c
+    float c_lo;                                  // the exact product minus c
+    double scale, dc, inv_c;                     // dc: c_lo in 64 bits; inv_c = 1 / c
 };
 
 // the column row n chose, -1 where it takes no part
@@ -90,104 +91,179 @@ struct Fp16 {
 };
 
 // ---------------------------------------------------------------------------
-// Part of a row's softmax: m = max z, s = sum 2^t, u = sum t 2^t over the elements seen, t = c z - K with the shift
-// K = fl(c m).  K need not be exact: every use takes the same K, and the error of c against scale log2 e (2^-24 of t at
-// worst, the same sign all along a row) is made up for in the log-sum-exp to first order, ln 2 (exact c - c) E[z] with E[z]
-// from u.  Over sums of thousands of log-probabilities it would otherwise show.
-// Rows of nothing but values near the type's lowest would overflow c m; they are `far`: t = c (z - m).
-// Elements of minus infinity add 0 (their t enters u clamped); a NaN stays in s.
+// The softmax of a row in powers of two:  2^t with t = c z - K,  K = fl(c m), m the maximum.  K need not be c m exactly: every
+// use of the row takes the same K.  From |c m| = 2^30 on that would overflow; but there neighbouring numbers of any type
+// are 64 apart in c z, so that only elements equal to the maximum count, and a power of two in place of c that puts c m at
+// 2^31 makes K exact and keeps the others at 2^-128 (`far`).
 // ---------------------------------------------------------------------------
-struct Part { float m, s, u; };
-constexpr float FAR = 1e30f, T_MIN = -1e4f;
-__device__ __forceinline__ float shift_of(float m, float c) { return m == -INFINITY ? 0.0f : m * c; }
-__device__ __forceinline__ bool is_far(float K) { return fabsf(K) > FAR; }
-__device__ __forceinline__ float exponent_of(float z, float m, float K, float c) { return is_far(K) ? (z - m) * c : fmaf(z, c, -K); }
+struct Shift { float c, K; };
+constexpr float FAR = 0x1p30f, T_MIN = -1e4f;
+__device__ __forceinline__ bool is_far(float m, float c) { return !(fabsf(m * c) < FAR) && m != -INFINITY; }
+__device__ __forceinline__ Shift shift_of(float m, float c)
+{
+    if (m == -INFINITY) return Shift{c, 0.0f};                          // nothing seen yet, or nothing allowed
+    if (!is_far(m, c)) return Shift{c, m * c};
+    if (m == INFINITY) return Shift{1.0f, m};                           // (inf - inf: the row becomes NaN)
+    const int e = (int)((__float_as_uint(m) >> 23) & 0xff) - 127;
+    const float p = __builtin_amdgcn_ldexpf(1.0f, 31 - e);
+    return Shift{p, m * p};
+}
 
-// p's sums moved to the shift of a larger maximum
-__device__ __forceinline__ void rescale(Part& p, float m, float c)
+// Sums over part of a row: s = sum 2^t, and beside it either u = sum t 2^t (the entropy) or, `fine`, u = sum r 2^t with r what
+// rounding took from the exponents: there t = fl(c x), x = z - m, and r = c x - t with c to 48 bits.  r matters where thousands
+// of log-probabilities are summed and two such sums subtracted.  Elements of minus infinity add 0 (their t or r enters u
+// clamped); a NaN stays in s.
+struct Part { float m, s, u; };
+template <bool FINE>
+__device__ __forceinline__ void rescale(Part& p, float m, float c, float c_lo)      // to a larger maximum
 {
     if (p.m == m || p.m == -INFINITY) { p.m = m; return; }
-    const float K0 = shift_of(p.m, c), K1 = shift_of(m, c);
-    const float d = fmaxf((is_far(K0) || is_far(K1)) ? (p.m - m) * c : K0 - K1, T_MIN);
+    const float x = p.m - m;
+    float d, r = 0.0f;
+    if (FINE) { d = fmaxf(x * c, T_MIN); r = __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -d)), -1.0f, 1.0f); }
+    else d = fmaxf(is_far(p.m, c) || is_far(m, c) ? x * c : p.m * c - m * c, T_MIN);
     const float f = __builtin_amdgcn_exp2f(d);
-    p.u = f * fmaf(p.s, d, p.u);
+    p.u = f * fmaf(p.s, FINE ? r : d, p.u);
     p.s *= f;
     p.m = m;
 }
-__device__ __forceinline__ Part joined(Part a, Part b, float c)
+template <bool FINE>
+__device__ __forceinline__ Part joined(Part a, Part b, float c, float c_lo)
 {
     const float m = fmaxf(a.m, b.m);
-    rescale(a, m, c); rescale(b, m, c);
+    rescale<FINE>(a, m, c, c_lo); rescale<FINE>(b, m, c, c_lo);
     return Part{m, a.s + b.s, a.u + b.u};
 }
-template <int N>
-__device__ __forceinline__ void add_elements(Part& p, const float (&z)[N], float c)
+// elements at shift k (coarse) or maximum m (fine)
+template <bool FINE, int N>
+__device__ __forceinline__ void add_at(Part& p, const float (&z)[N], float m, const Shift& k, float c, float c_lo)
 {
-    float m = z[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
-    m = fmaxf(m, p.m);                                                  // (fmaxf passes over a NaN)
-    if (m > p.m) rescale(p, m, c);
-    const float K = shift_of(p.m, c);
-    if (is_far(K)) {
-        const float m0 = p.m;
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const float t = (z[i] - m0) * c, e = __builtin_amdgcn_exp2f(t); p.s += e; p.u = fmaf(e, fmaxf(t, T_MIN), p.u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const float t = fmaf(z[i], c, -K), e = __builtin_amdgcn_exp2f(t); p.s += e; p.u = fmaf(e, fmaxf(t, T_MIN), p.u); }
+    for (int i = 0; i < N; ++i) {
+        if (FINE) {
+            const float x = z[i] - m, t = x * c, e = __builtin_amdgcn_exp2f(t);
+            p.s += e;
+            p.u = fmaf(e, __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -t)), -1.0f, 1.0f), p.u);
+        } else {
+            const float t = fmaf(z[i], k.c, -k.K), e = __builtin_amdgcn_exp2f(t);
+            p.s += e;
+            p.u = fmaf(e, fmaxf(t, T_MIN), p.u);
+        }
     }
 }
-__device__ __forceinline__ Part wave_joined(Part p, float c, int lanes = 64)
+template <int N>
+__device__ __forceinline__ float max_of(const float (&z)[N], float m)   // (passes over a NaN)
 {
-    for (int off = 1; off < lanes; off <<= 1) {
-        Part q{__shfl_xor(p.m, off, 64), __shfl_xor(p.s, off, 64), __shfl_xor(p.u, off, 64)};
-        p = joined(p, q, c);
-    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, z[i]);
+    return m;
+}
+template <bool FINE, int N>
+__device__ __forceinline__ void add_elements(Part& p, const float (&z)[N], float c, float c_lo)
+{
+    const float m = max_of(z, p.m);
+    if (m > p.m) rescale<FINE>(p, m, c, c_lo);
+    add_at<FINE>(p, z, m == -INFINITY ? 0.0f : m, shift_of(m, c), c, c_lo);
+}
+template <bool FINE>
+__device__ __forceinline__ Part lanes_joined(Part p, float c, float c_lo, int lanes)
+{
+    for (int off = 1; off < lanes; off <<= 1) p = joined<FINE>(p, Part{__shfl_xor(p.m, off, 64), __shfl_xor(p.s, off, 64), __shfl_xor(p.u, off, 64)}, c, c_lo);
     return p;
 }
 
-// a whole row: log-sum-exp, entropy, log-probability of an element, and 1 / s for the gradient
+// ---- one row's numbers in 64 bits --------------------------------------------------------------------------------
+__device__ __forceinline__ double reciprocal(double x)
+{
+    double r = __builtin_amdgcn_rcp(x);
+    r = fma(fma(-x, r, 1.0), r, r);
+    return fma(fma(-x, r, 1.0), r, r);
+}
+// ln x of a sum of exponentials: mantissa in (sqrt 1/2, sqrt 2], 2 atanh((m - 1) / (m + 1)) as a series to the 15th power
+// (off by 1e-14 at most).  Other x (zero, NaN, infinite) as log has it.
+__device__ __forceinline__ double log_of_sum(double x)
+{
+    if (!(x > 1e-30 && x < 1e30)) return x == 0.0 ? -INFINITY : x == INFINITY ? INFINITY : NAN;
+    const uint64_t b = __double_as_longlong(x);
+    int e = (int)(b >> 52) - 1023;
+    double m = __longlong_as_double((b & 0xfffffffffffffull) | 0x3ff0000000000000ull);
+    if (m > 1.4142135623730951) { m *= 0.5; e += 1; }
+    const double f = (m - 1.0) * reciprocal(m + 1.0), g = f * f;
+    double p = 1.0 / 15;
+    p = fma(p, g, 1.0 / 13); p = fma(p, g, 1.0 / 11); p = fma(p, g, 1.0 / 9); p = fma(p, g, 1.0 / 7);
+    p = fma(p, g, 1.0 / 5); p = fma(p, g, 1.0 / 3); p = fma(p, g, 1.0);
+    return fma((double)e, LN2, 2.0 * f * p);
+}
+// e^x to single precision's last place, for x in 64 bits
+__device__ __forceinline__ float exp_of(double x)
+{
+    double t = x * LOG2E;
+    t = t > 300.0 ? 300.0 : t < -300.0 ? -300.0 : t;                    // (NaN stays)
+    const double i = rint(t);
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(t - i)), (int)i);
+}
+
 struct RowSum {
-    double lse, entropy, log_s;
-    float m, K, inv_s;
-    bool empty;                                                         // all of it minus infinity
+    double lse, entropy, log_s;                  // log_s: with the shift's own c
+    float m; Shift k;
+    float inv_s;
+    bool far, empty;                             // empty: all of it minus infinity
 };
+template <bool FINE>
 __device__ __forceinline__ RowSum finish_row(const Part& p, const Rows& r)
 {
-    RowSum x;
-    x.m = p.m; x.K = shift_of(p.m, r.c);
+    RowSum x{};
+    x.m = p.m; x.far = is_far(p.m, r.c);
     x.empty = p.m == -INFINITY && p.s == 0.0f;
-    const double s = (double)p.s, mean_t = (double)p.u / s;             // E[t]
-    const double log_s = log(s);                                        // with c for scale log2 e, as the exponents have it
-    if (is_far(x.K)) x.lse = r.scale * (double)p.m + log_s;
-    else x.lse = LN2 * ((double)x.K + r.dc * ((mean_t + (double)x.K) / (double)r.c)) + log_s;
-    x.entropy = log_s - LN2 * mean_t;
-    x.log_s = log_s;
-    x.inv_s = (float)exp(-log_s);
-    if (x.empty) { x.lse = -INFINITY; x.entropy = 0.0; x.inv_s = 0.0f; x.log_s = 0.0; }
+    x.k = shift_of(p.m, r.c);
+    if (x.empty) { x.lse = -INFINITY; return x; }
+    if (FINE) {
+        const double s = fma(LN2, (double)p.u, (double)p.s);
+        x.log_s = log_of_sum(s);
+        x.lse = fma(r.scale, (double)p.m, x.log_s);
+        // the shift of the gradient: 2^(c z - K) / s' with K = fl(c m)
+        x.inv_s = (float)(reciprocal(s) * (x.far ? 1.0 : (double)exp_of(((double)x.k.K - (double)r.c * (double)p.m) * LN2)));
+        return x;
+    }
+    const double s = (double)p.s, inv = reciprocal(s), mean_t = (double)p.u * inv;      // E[t]
+    x.log_s = log_of_sum(s);
+    // c stands for scale log2 e (off by 2^-25 of it): to first order that adds  ln 2 (exact c - c) E[z]  to the log-sum-exp
+    if (x.far) x.lse = fma(r.scale, (double)p.m, x.log_s);
+    else x.lse = LN2 * ((double)x.k.K + r.dc * ((mean_t + (double)x.k.K) * r.inv_c)) + x.log_s;
+    x.entropy = x.log_s - LN2 * fmax(mean_t, (double)T_MIN);
+    x.inv_s = (float)inv;
     return x;
 }
+template <bool FINE>
 __device__ __forceinline__ double logp_of(const RowSum& x, float z, const Rows& r)
 {
     if (x.empty) return -INFINITY;
-    if (is_far(x.K)) return r.scale * ((double)z - (double)x.m) - x.log_s;
+    if (FINE || x.far) return r.scale * ((double)z - (double)x.m) - x.log_s;
     return r.scale * (double)z - x.lse;
 }
 
 // Gradient of one row: element j gets 2^t (a0 + a1 t), and the target `to_target` more.  From  g ([j = a] - p_j) - e p_j (log p_j + H)
 // with p_j = 2^t / s, log p_j = ln 2 t - log s:  a0 = (-g - e (H - log s)) / s,  a1 = -e ln 2 / s.
-struct RowGrad { float m, K, a0, a1, to_target; int target; };
+struct RowGrad { Shift k; float a0, a1, to_target; int target; };
 __device__ __forceinline__ RowGrad row_gradient(const RowSum& x, double g, double e, int target, double scale)
 {
     RowGrad q;
-    q.m = x.m; q.K = x.K; q.target = target;
+    q.k = x.k; q.target = target;
     const double k = scale * (double)x.inv_s;
     q.a0 = (float)(k * (-g - (e != 0.0 ? e * (x.entropy - x.log_s) : 0.0)));
     q.a1 = (float)(-k * e * LN2);
     q.to_target = (float)(scale * g);
     if (x.empty) q.a0 = q.a1 = q.to_target = 0.0f;
     return q;
+}
+template <bool ENT, int N>
+__device__ __forceinline__ void gradient_of(const RowGrad& q, const float (&z)[N], float (&d)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = fmaf(z[i], q.k.c, -q.k.K);
+        d[i] = __builtin_amdgcn_exp2f(t) * (ENT ? fmaf(q.a1, fmaxf(t, T_MIN), q.a0) : q.a0);
+    }
 }
 
 // ---- sequences over rows -----------------------------------------------------------------------------------------

@@ -1,158 +1,19 @@
 // Operators of token policies on rows of logits: log-probabilities and their backward pass, the clipped policy loss, and
-// the loss over pairs of sequences.  The mathematics stands in tokens.h (one row) and at the kernels below.
-//   row_sums         a workgroup per row: log-sum-exp, entropy, log-probability of the target
-//   row_gradients    a workgroup per row: d / d logits from a row's coefficients
-//   weight_sums      partial sums of the rows' (pairs') weights
-//   policy_rows      the clipped loss: coefficients of a row's gradient and the sums that are reported
-//   pair_sums        the pairs: summed log ratios, coefficients of their rows
-//   finish_stats     adds the workgroups' sums in a fixed order
+// the loss over pairs of sequences.  The mathematics of a row stands in tokens.h, that of the losses at policy_row and
+// pair_sums.  Three things are done with a row -- its sums, its gradient from given coefficients, and both with the clipped
+// loss between them -- and each comes in three forms by the length of a row:
+//   lanes_*    short rows: 1 to 64 lanes hold a row in registers, 64 / lanes rows to a wavefront
+//   block_sums, block_gradients   a workgroup streams a row
+//   block_policy                  a workgroup holds a row in registers between its sums and its gradient
+// and   weight_sums   partial sums of the rows' (pairs') weights
+//       pair_sums     the pairs: summed log ratios, coefficients of their rows
+//       finish_stats  adds the workgroups' sums in a fixed order
 #include <math.h>
 #include "tokens.h"
 
 namespace ank {
 
-// what the first pass leaves of a row for the second
-struct __align__(16) RowWs { double lp, entropy, log_s; float m, K, inv_s; int target; int empty, pad; };
 struct Partial { double v[STATS]; };
-
-__device__ __forceinline__ Part block_joined(Part p, float c, Part* lds)
-{
-    p = wave_joined(p, c);
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    if (waves == 1) return p;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[wave] = p;
-    __syncthreads();
-    Part q = lds[0];
-    for (int w = 1; w < waves; ++w) q = joined(q, lds[w], c);
-    return q;
-}
-
-// elements [begin, end) of a row, shared out over the workgroup
-template <class E>
-__device__ __forceinline__ Part row_part(const typename E::T* row, int begin, int end, float c)
-{
-    Part p{-INFINITY, 0.0f, 0.0f};
-    const int vecs = (end - begin) / E::N;
-    for (int v = threadIdx.x; v < vecs; v += blockDim.x) {
-        float z[E::N];
-        E::unpack(*reinterpret_cast<const u32x4_any*>(row + begin + v * E::N), z);
-        add_elements(p, z, c);
-    }
-    for (int j = begin + vecs * E::N + threadIdx.x; j < end; j += blockDim.x) {
-        const float z[1] = {E::get(row + j)};
-        add_elements(p, z, c);
-    }
-    return p;
-}
-
-struct SumArgs {
-    Rows r;
-    const float* weight;                         // rows of weight 0 take no part (null: 1)
-    float *logp, *lse, *entropy;                 // each may be null
-    RowWs* ws;                                   // may be null
-    float* coef;                                 // may be null: set to 0 (pair_sums fills in the rows of its sequences)
-};
-
-// ---------------------------------------------------------------------------
-// One pass over a row with running maximum and sums.  Bound by the read.
-// ---------------------------------------------------------------------------
-template <class E>
-__global__ __launch_bounds__(WG) void row_sums(const SumArgs a)
-{
-    __shared__ Part lds[WG / 64];
-    for (int64_t n = blockIdx.x; n < a.r.rows; n += gridDim.x) {
-        int target = row_target(a.r, n);
-        if (a.weight && a.weight[n] == 0.0f) target = -1;
-        const typename E::T* row = static_cast<const typename E::T*>(a.r.logits) + n * a.r.stride;
-        Part p{-INFINITY, 0.0f, 0.0f};
-        if (target >= 0) p = block_joined(row_part<E>(row, 0, a.r.V, a.r.c), a.r.c, lds);
-        if (threadIdx.x == 0) {
-            RowSum x{};
-            double lp = 0.0;
-            if (target >= 0) { x = finish_row(p, a.r); lp = logp_of(x, E::get(row + target), a.r); }
-            if (a.logp) a.logp[n] = (float)lp;
-            if (a.lse) a.lse[n] = (float)x.lse;
-            if (a.entropy) a.entropy[n] = (float)x.entropy;
-            if (a.ws) a.ws[n] = RowWs{lp, x.entropy, x.log_s, x.m, x.K, x.inv_s, target, x.empty, 0};
-            if (a.coef) a.coef[n] = 0.0f;
-        }
-    }
-}
-
-// the coefficients of row n's gradient, and whether it has one
-struct GradArgs {
-    Rows r;
-    void* out; int64_t out_stride;
-    const RowWs* ws;                             // log-sum-exp and the like of the first pass; null: from the caller's lse
-    const float *lse, *entropy, *to_logp, *to_entropy;   // the caller's (to_entropy may be null); to_logp also with ws
-    const double* inv;                           // factor of to_logp and to_entropy (null: 1)
-};
-__device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
-{
-    double g = a.to_logp[n], e = a.to_entropy ? a.to_entropy[n] : 0.0;
-    if (a.inv) { g *= *a.inv; e *= *a.inv; }
-    RowSum x;
-    int target;
-    if (a.ws) {
-        const RowWs w = a.ws[n];
-        x.entropy = w.entropy; x.log_s = w.log_s; x.m = w.m; x.K = w.K; x.inv_s = w.inv_s; x.empty = w.empty != 0;
-        target = w.target;
-    } else {
-        // p_j = 2^(c z - K) (1 / s) with K = fl(lse log2 e) and the rest of lse in s
-        target = row_target(a.r, n);
-        const double lse = target >= 0 ? (double)a.lse[n] : 0.0, k = lse * LOG2E;
-        x.empty = lse == -INFINITY;
-        x.m = (float)(lse / a.r.scale); x.K = (float)k;
-        x.log_s = x.empty || is_far(x.K) ? 0.0 : (k - (double)x.K) * LN2;
-        x.inv_s = (float)exp(-x.log_s);
-        x.entropy = e != 0.0 && target >= 0 ? (double)a.entropy[n] : 0.0;
-    }
-    return row_gradient(x, g, e, target, a.r.scale);
-}
-
-template <int N, bool ENT>
-__device__ __forceinline__ void gradient_of(const RowGrad& q, float c, int j0, const float (&z)[N], float (&d)[N])
-{
-    if (is_far(q.K)) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const float t = (z[i] - q.m) * c; d[i] = __builtin_amdgcn_exp2f(t) * (ENT ? fmaf(q.a1, fmaxf(t, T_MIN), q.a0) : q.a0); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const float t = fmaf(z[i], c, -q.K); d[i] = __builtin_amdgcn_exp2f(t) * (ENT ? fmaf(q.a1, fmaxf(t, T_MIN), q.a0) : q.a0); }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) d[i] += j0 + i == q.target ? q.to_target : 0.0f;
-}
-
-// ---------------------------------------------------------------------------
-// d / d logits of a row, element by element.  Bound by the read and the write.
-// ---------------------------------------------------------------------------
-template <class E, bool ENT>
-__global__ __launch_bounds__(WG) void row_gradients(const GradArgs a)
-{
-    typedef typename E::T T;
-    for (int64_t n = blockIdx.x; n < a.r.rows; n += gridDim.x) {
-        const RowGrad q = grad_of_row(a, n);
-        const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
-        T* out = static_cast<T*>(a.out) + n * a.out_stride;
-        const int V = a.r.V, vecs = V / E::N;
-        const bool zero = q.target < 0;
-        for (int v = threadIdx.x; v < vecs; v += blockDim.x) {
-            float z[E::N], d[E::N] = {};
-            if (!zero) {
-                E::unpack(*reinterpret_cast<const u32x4_any*>(row + v * E::N), z);
-                gradient_of<E::N, ENT>(q, a.r.c, v * E::N, z, d);
-            }
-            *reinterpret_cast<u32x4_any*>(out + v * E::N) = E::pack(d);
-        }
-        for (int j = vecs * E::N + threadIdx.x; j < V; j += blockDim.x) {
-            float z[1], d[1] = {0.0f};
-            if (!zero) { z[0] = E::get(row + j); gradient_of<1, ENT>(q, a.r.c, j, z, d); }
-            E::put(out + j, d[0]);
-        }
-    }
-}
 
 // ---- sums in a fixed order ---------------------------------------------------------------------------------------
 __device__ __forceinline__ double wave_sum(double v)
@@ -180,34 +41,129 @@ __device__ __forceinline__ void block_partial(const double (&v)[STATS], double* 
         for (int k = 0; k < STATS; ++k) out->v[k] = s[k];
 }
 
+// What a mean is taken over: the given norm, or the sum of the weights -- of parts that weight_sums left, or of the rows
+// themselves where they are few enough for every workgroup to add them up beside its first loads (a launch less).
+struct Norm { double norm; const double* parts; int n_parts; const float* weight; int inline_rows; };
+constexpr int INLINE_ROWS = 2048;
+__device__ __forceinline__ double weight_of(const Rows& r, const float* weight, int64_t n) { return row_target(r, n) < 0 ? 0.0 : weight ? (double)weight[n] : 1.0; }
+// the share of it that this thread of `threads` adds up; the sum over all threads is W
+__device__ __forceinline__ double weight_share(const Norm& w, const Rows& r, int thread, int threads)
+{
+    if (w.norm != 0.0) return thread == 0 ? w.norm : 0.0;
+    double s = 0.0;
+    for (int i = thread; i < w.n_parts; i += threads) s += w.parts[i];
+    for (int i = thread; i < w.inline_rows; i += threads) s += weight_of(r, w.weight, i);
+    return s;
+}
+
 // partial sums of the weights of the rows (target in range) or pairs that take part
 __global__ __launch_bounds__(WG) void weight_sums(const Rows r, const int64_t n, const float* weight, const bool pairs, double* parts)
 {
     __shared__ double lds[WG / 64];
     double s = 0.0;
     for (int64_t i = (int64_t)blockIdx.x * WG + threadIdx.x; i < n; i += (int64_t)gridDim.x * WG)
-        if (pairs || row_target(r, i) >= 0) s += weight ? (double)weight[i] : 1.0;
+        s += pairs ? (double)weight[i] : weight_of(r, weight, i);
     s = block_sum(s, lds);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
-// what a mean is taken over: the given norm, or the sum of the weights
-struct Norm { double norm; const double* parts; int n_parts; };
-__device__ __forceinline__ double weight_total(const Norm& w)
+// means over W of the summed statistics; slot 0 becomes the loss
+struct FinishArgs { const Partial* parts; int n_parts; Rows r; Norm norm; float* stats; double kl, ent; int policy; };
+__device__ __forceinline__ void finish(const FinishArgs& a, double* lds)
 {
-    if (w.norm != 0.0) return w.norm;
-    double s = 0.0;
-    for (int i = threadIdx.x & 63; i < w.n_parts; i += 64) s += w.parts[i];
-    return wave_sum(s);
+    double v[STATS] = {};
+    for (int i = threadIdx.x; i < a.n_parts; i += blockDim.x)
+#pragma unroll
+        for (int k = 0; k < STATS; ++k) v[k] += a.parts[i].v[k];
+#pragma unroll
+    for (int k = 0; k < STATS; ++k) v[k] = block_sum(v[k], lds);
+    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, blockDim.x), lds), inv = W != 0.0 ? 1.0 / W : 0.0;
+    if (threadIdx.x != 0) return;
+    double m[STATS];
+#pragma unroll
+    for (int k = 0; k < STATS; ++k) m[k] = W != 0.0 ? v[k] * inv : 0.0;
+    if (a.policy) m[0] = m[1] + (a.kl != 0.0 ? a.kl * m[2] : 0.0) - (a.ent != 0.0 ? a.ent * m[3] : 0.0);
+    m[5] = a.policy ? m[5] : W;                                         // pairs: loss, [h > 0], first, second, h, W, pairs, tokens
+    m[6] = a.policy ? W : v[6];
+    m[7] = v[7];
+#pragma unroll
+    for (int k = 0; k < STATS; ++k) a.stats[k] = (float)m[k];
+}
+constexpr int FINISH_WG = 1024;
+__global__ __launch_bounds__(FINISH_WG) void finish_stats(const FinishArgs a)
+{
+    __shared__ double lds[FINISH_WG / 64];
+    finish(a, lds);
+}
+
+// ---- what becomes of a row's sums -----------------------------------------------------------------------------------
+// what the first pass over pairs leaves of a row for the second
+struct RowWs { double lp; Shift k; float inv_s; int target; };
+
+struct SumArgs {
+    Rows r;
+    float *logp, *lse, *entropy;                 // each may be null
+    RowWs* ws;                                   // may be null
+    float* coef;                                 // may be null: set to 0 (pair_sums fills in the rows of its sequences)
+};
+template <bool FINE>
+__device__ __forceinline__ void store_sums(const SumArgs& a, int64_t n, const Part& p, int target, float chosen)
+{
+    RowSum x{};
+    double lp = 0.0;
+    if (target >= 0) { x = finish_row<FINE>(p, a.r); lp = logp_of<FINE>(x, chosen, a.r); }
+    if (a.logp) a.logp[n] = (float)lp;
+    if (a.lse) a.lse[n] = (float)x.lse;
+    if (a.entropy) a.entropy[n] = (float)x.entropy;
+    if (a.ws) a.ws[n] = RowWs{lp, x.k, x.empty ? 0.0f : x.inv_s, target};
+    if (a.coef) a.coef[n] = 0.0f;
+}
+
+struct GradArgs {
+    Rows r;
+    void* out; int64_t out_stride;
+    const RowWs* ws;                             // of the first pass; null: from the caller's lse
+    const float *lse, *entropy, *to_logp, *to_entropy;   // the caller's (to_entropy may be null); to_logp also with ws
+    FinishArgs fin;                              // stats not null: a workgroup more finishes the statistics
+};
+__device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
+{
+    RowSum x{};
+    if (a.ws) {
+        const RowWs w = a.ws[n];
+        x.k = w.k; x.inv_s = w.inv_s;
+        return row_gradient(x, a.to_logp[n], 0.0, w.target, a.r.scale);
+    }
+    const int target = row_target(a.r, n);
+    if (target < 0) return row_gradient(x, 0.0, 0.0, -1, 0.0);
+    // p_j = 2^(c z - K) / s with K = fl(lse log2 e) and the rest of lse in s.  (A log-sum-exp of 2^30 and more has no room for
+    // probabilities: its neighbours are 64 apart.  The maximum's is 1 and nothing overflows.)
+    const double e = a.to_entropy ? a.to_entropy[n] : 0.0, lse = a.lse[n], k = lse * LOG2E, zc = lse / a.r.scale;
+    x.empty = lse == -INFINITY;
+    x.k = Shift{a.r.c, x.empty ? 0.0f : (float)k};
+    double rest = x.empty ? 0.0 : k - (double)x.k.K;
+    if (fabs(k) >= (double)FAR && !x.empty) {
+        rest = 0.0;
+        if (fabs(zc) < 3.4028234663852886e38) {
+            const float m = (float)zc, p = __builtin_amdgcn_ldexpf(1.0f, 24 - ((int)((__float_as_uint(m) >> 23) & 0xff) - 127));
+            x.k = Shift{p, m * p};
+        }
+    }
+    x.log_s = rest * LN2;
+    x.inv_s = exp_of(-x.log_s);
+    x.entropy = e != 0.0 ? (double)a.entropy[n] : 0.0;
+    return row_gradient(x, a.to_logp[n], e, target, a.r.scale);
 }
 
 // ---------------------------------------------------------------------------
-// The clipped loss of one row, everything in 64 bits: which side of a clipping border a ratio lies on hangs on lp.
+// The clipped loss of one row.  Which side of a clipping border a ratio lies on hangs on lp, so the difference of the
+// log-probabilities is compared with the borders' logarithms in 64 bits.
 //   dL/dlp = w (-A r [r A <= clipped A] + kl_coef (1 - e^d)),  dL/dH = -entropy_coef w    (both without 1 / W)
 // ---------------------------------------------------------------------------
 struct PolicyCfg {
     const float *old, *adv, *ref, *weight;
-    double low, high, kl, ent, grad_scale;
+    double log_low, log_high;                    // ln(1 - clip_low), ln(1 + clip_high)
+    double low, high, kl, ent, grad_scale;       // low = 1 - clip_low, high = 1 + clip_high
 };
 struct PolicyRow { double g, e, policy, kl, entropy, clipped, ratio, w; };
 __device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, int64_t n, double lp, double entropy, bool empty)
@@ -215,15 +171,23 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, int64_t n, d
     PolicyRow x{};
     x.w = a.weight ? (double)a.weight[n] : 1.0;
     if (empty) return x;
-    const double A = a.adv[n], r = exp(lp - (double)a.old[n]);
-    const double plain = r * A, clip = fmin(fmax(r, 1.0 - a.low), 1.0 + a.high) * A;
-    const bool inside = plain <= clip || plain != plain;                // a NaN stays in the gradient
-    x.policy = -(inside ? plain : clip); x.clipped = inside ? 0.0 : 1.0; x.ratio = r; x.entropy = entropy;
-    x.g = inside ? -plain : 0.0;
+    const double A = a.adv[n], diff = lp - (double)a.old[n], r = (double)exp_of(diff);
+    const bool clipped = (A > 0.0 && diff > a.log_high) || (A < 0.0 && diff < a.log_low);      // (a NaN stays in the gradient)
+    x.policy = clipped ? -(A > 0.0 ? a.high : a.low) * A : -r * A;
+    x.clipped = clipped ? 1.0 : 0.0; x.ratio = r; x.entropy = entropy;
+    x.g = clipped ? 0.0 : -r * A;
     if (a.ref) {
-        const double d = (double)a.ref[n] - lp, e = exp(d);
-        x.kl = e - d - 1.0;
-        if (a.kl != 0.0) x.g += a.kl * (1.0 - e);
+        // e^d - 1 and e^d - 1 - d: their series where they would cancel
+        const double d = (double)a.ref[n] - lp;
+        double e1, e2;
+        if (fabs(d) < 0.5) {
+            double p = 1.0 / 39916800;
+            p = fma(p, d, 1.0 / 3628800); p = fma(p, d, 1.0 / 362880); p = fma(p, d, 1.0 / 40320); p = fma(p, d, 1.0 / 5040);
+            p = fma(p, d, 1.0 / 720); p = fma(p, d, 1.0 / 120); p = fma(p, d, 1.0 / 24); p = fma(p, d, 1.0 / 6); p = fma(p, d, 0.5);
+            e2 = p * d * d; e1 = e2 + d;
+        } else { e1 = (double)exp_of(d) - 1.0; e2 = e1 - d; }
+        x.kl = e2;
+        if (a.kl != 0.0) x.g -= a.kl * e1;
     }
     x.g *= x.w; x.e = -a.ent * x.w;
     return x;
@@ -232,58 +196,367 @@ __device__ __forceinline__ void add_stats(double (&v)[STATS], const PolicyRow& x
 {
     v[1] += x.w * x.policy; v[2] += x.w * x.kl; v[3] += x.w * x.entropy; v[4] += x.w * x.clipped; v[5] += x.w * x.ratio; v[6] += x.w; v[7] += 1.0;
 }
-
 struct PolicyArgs {
+    Rows r;
     PolicyCfg p;
-    int64_t rows;
-    const RowWs* ws;
-    float *to_logp, *to_entropy;
     Norm norm;
+    float* logp;                                 // may be null
+    void* out; int64_t out_stride;               // out null: the loss alone
     Partial* parts;
 };
-__global__ __launch_bounds__(WG) void policy_rows(const PolicyArgs a)
+__device__ __forceinline__ int policy_target(const PolicyArgs& a, int64_t n)
 {
-    __shared__ double lds[WG / 64];
-    const double W = weight_total(a.norm), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
-    double v[STATS] = {};
-    for (int64_t n = (int64_t)blockIdx.x * WG + threadIdx.x; n < a.rows; n += (int64_t)gridDim.x * WG) {
-        const RowWs w = a.ws[n];
-        float g = 0.0f, e = 0.0f;
-        if (w.target >= 0) {
-            const PolicyRow x = policy_row(a.p, n, w.lp, w.entropy, w.empty != 0);
-            add_stats(v, x);
-            g = (float)(x.g * inv); e = (float)(x.e * inv);
-        }
-        a.to_logp[n] = g; a.to_entropy[n] = e;
-    }
-    block_partial(v, lds, a.parts + blockIdx.x);
+    const int t = row_target(a.r, n);
+    return a.p.weight && a.p.weight[n] == 0.0f ? -1 : t;
 }
 
-// means over W of the summed statistics; slot 0 becomes the loss
-struct FinishArgs { const Partial* parts; int n_parts; Norm norm; float* stats; double kl, ent; int policy; };
-__global__ __launch_bounds__(WG) void finish_stats(const FinishArgs a)
+// ---------------------------------------------------------------------------
+// Short rows.  `lanes` lanes (a power of two up to 64) hold a row, NE elements each: VECTOR -- 16 bytes at a time, piece k of
+// lane l at vector k lanes + l; else one element at a time, element k of lane l in column k lanes + l.  Everything of a row
+// happens in registers; all its lanes carry out the row's 64-bit arithmetic together.
+// ---------------------------------------------------------------------------
+enum { DO_SUMS, DO_GRADIENT, DO_POLICY };
+struct LaneArgs { int lanes; SumArgs s; GradArgs g; PolicyArgs p; };
+
+template <class E, int NE, bool VECTOR>
+struct LaneRow {
+    typedef typename E::T T;
+    static __device__ __forceinline__ void load(const T* row, int V, int lanes, int l, float (&z)[NE])
+    {
+        if (VECTOR) {
+#pragma unroll
+            for (int k = 0; k < NE / E::N; ++k) {
+                const int j = (k * lanes + l) * E::N;
+                if (j + E::N <= V) {
+                    float f[E::N];
+                    E::unpack(*reinterpret_cast<const u32x4_any*>(row + j), f);
+#pragma unroll
+                    for (int i = 0; i < E::N; ++i) z[k * E::N + i] = f[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < E::N; ++i) z[k * E::N + i] = j + i < V ? E::get(row + j + i) : -INFINITY;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; z[k] = j < V ? E::get(row + j) : -INFINITY; }
+        }
+    }
+    // the gradient d, and `more` at column `target`; d null (zero): zeros
+    static __device__ __forceinline__ void store(T* out, int V, int lanes, int l, float (&d)[NE], int target, float more)
+    {
+#pragma unroll
+        for (int k = 0; k < NE; ++k) {
+            const int j = VECTOR ? ((k / E::N) * lanes + l) * E::N + k % E::N : k * lanes + l;
+            d[k] += j == target ? more : 0.0f;
+        }
+        if (VECTOR) {
+#pragma unroll
+            for (int k = 0; k < NE / E::N; ++k) {
+                const int j = (k * lanes + l) * E::N;
+                if (j + E::N <= V) {
+                    float f[E::N];
+#pragma unroll
+                    for (int i = 0; i < E::N; ++i) f[i] = d[k * E::N + i];
+                    *reinterpret_cast<u32x4_any*>(out + j) = E::pack(f);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < E::N; ++i) if (j + i < V) E::put(out + j + i, d[k * E::N + i]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; if (j < V) E::put(out + j, d[k]); }
+        }
+    }
+};
+template <bool FINE, int NE>
+__device__ __forceinline__ Part lanes_part(const float (&z)[NE], const Rows& r, int lanes)
 {
+    float m = max_of(z, -INFINITY);
+    for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    Part p{m, 0.0f, 0.0f};
+    add_at<FINE>(p, z, m == -INFINITY ? 0.0f : m, shift_of(m, r.c), r.c, r.c_lo);
+    for (int off = 1; off < lanes; off <<= 1) { p.s += __shfl_xor(p.s, off, 64); p.u += __shfl_xor(p.u, off, 64); }
+    return p;
+}
+
+template <class E, int DO, int NE, bool VECTOR, bool FINE>
+__global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs a)
+{
+    typedef typename E::T T;
+    typedef LaneRow<E, NE, VECTOR> L;
     __shared__ double lds[WG / 64];
-    double v[STATS] = {};
-    for (int i = threadIdx.x; i < a.n_parts; i += WG)
-        for (int k = 0; k < STATS; ++k) v[k] += a.parts[i].v[k];
-    for (int k = 0; k < STATS; ++k) v[k] = block_sum(v[k], lds);
-    const double W = weight_total(a.norm), inv = W != 0.0 ? 1.0 / W : 0.0;
-    if (threadIdx.x != 0) return;
-    double m[STATS];
-    for (int k = 0; k < STATS; ++k) m[k] = W != 0.0 ? v[k] * inv : 0.0;
-    if (a.policy) m[0] = m[1] + (a.kl != 0.0 ? a.kl * m[2] : 0.0) - (a.ent != 0.0 ? a.ent * m[3] : 0.0);
-    m[5] = a.policy ? m[5] : W;                                         // pairs: loss, [h > 0], first, second, h, W, pairs, tokens
-    m[6] = a.policy ? W : v[6];
-    m[7] = v[7];
-    for (int k = 0; k < STATS; ++k) a.stats[k] = (float)m[k];
+    const Rows& r = DO == DO_SUMS ? a.s.r : DO == DO_GRADIENT ? a.g.r : a.p.r;
+    const int lanes = a.lanes, l = threadIdx.x & (lanes - 1), per = WG / lanes, V = r.V;
+    if (DO == DO_GRADIENT && a.g.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.g.fin, lds); return; }
+    const int64_t grid = DO == DO_GRADIENT && a.g.fin.stats ? gridDim.x - 1 : gridDim.x;
+    double inv = 0.0, v[STATS] = {};
+    if (DO == DO_POLICY) {
+        const double W = block_sum(weight_share(a.p.norm, r, threadIdx.x, WG), lds);
+        inv = W != 0.0 ? a.p.p.grad_scale / W : 0.0;
+    }
+    for (int64_t base = (int64_t)blockIdx.x * per; base < r.rows; base += grid * per) {
+        const int64_t n = base + threadIdx.x / lanes;
+        const bool there = n < r.rows;
+        const T* row = static_cast<const T*>(r.logits) + (there ? n : 0) * r.stride;
+        int target = -1;
+        float z[NE], d[NE];
+        if (DO == DO_GRADIENT) {
+            if (!there) continue;
+            const RowGrad q = grad_of_row(a.g, n);
+            target = q.target;
+            if (target >= 0) { L::load(row, V, lanes, l, z); gradient_of<true>(q, z, d); }
+            else {
+#pragma unroll
+                for (int k = 0; k < NE; ++k) d[k] = 0.0f;
+            }
+            L::store(static_cast<T*>(a.g.out) + n * a.g.out_stride, V, lanes, l, d, target, q.to_target);
+            continue;
+        }
+        if (there) target = DO == DO_SUMS ? row_target(r, n) : policy_target(a.p, n);
+        if (target >= 0) L::load(row, V, lanes, l, z);
+        else {
+#pragma unroll
+            for (int k = 0; k < NE; ++k) z[k] = 0.0f;
+        }
+        const Part p = lanes_part<FINE>(z, r, lanes);
+        const float chosen = target >= 0 ? E::get(row + target) : 0.0f;
+        if (DO == DO_SUMS) {
+            if (there && l == 0) store_sums<FINE>(a.s, n, p, target, chosen);
+            continue;
+        }
+        RowGrad q{};
+        double lp = 0.0;
+        q.target = -1;
+        if (target >= 0) {
+            const RowSum x = finish_row<false>(p, r);
+            lp = logp_of<false>(x, chosen, r);
+            const PolicyRow y = policy_row(a.p.p, n, lp, x.entropy, x.empty);
+            if (l == 0) add_stats(v, y);
+            q = row_gradient(x, y.g * inv, y.e * inv, target, r.scale);
+        }
+        if (there && l == 0 && a.p.logp) a.p.logp[n] = (float)lp;
+        if (!there || !a.p.out) continue;
+        if (target >= 0) gradient_of<true>(q, z, d);
+        else {
+#pragma unroll
+            for (int k = 0; k < NE; ++k) d[k] = 0.0f;
+        }
+        L::store(static_cast<T*>(a.p.out) + n * a.p.out_stride, V, lanes, l, d, target, q.to_target);
+    }
+    if (DO == DO_POLICY) block_partial(v, lds, a.p.parts + blockIdx.x);
+}
+
+// ---------------------------------------------------------------------------
+// Long rows, a workgroup each.  Sums: one pass with every thread's own running maximum; bound by the read.
+// ---------------------------------------------------------------------------
+template <bool FINE>
+__device__ __forceinline__ Part block_joined(Part p, float c, float c_lo, Part* lds)
+{
+    p = lanes_joined<FINE>(p, c, c_lo, 64);
+    const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    __syncthreads();
+    if (lane == 0) lds[threadIdx.x >> 6] = p;
+    __syncthreads();
+    if (lane < waves) p = lds[lane];
+    return lanes_joined<FINE>(p, c, c_lo, waves);                       // (lane 0 has it; waves is a power of two)
+}
+template <class E, bool FINE>
+__global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
+{
+    __shared__ Part lds[16];
+    const int64_t n = blockIdx.x;
+    const int target = row_target(a.r, n), V = a.r.V, nt = blockDim.x;
+    const typename E::T* row = static_cast<const typename E::T*>(a.r.logits) + n * a.r.stride;
+    Part p{-INFINITY, 0.0f, 0.0f};
+    if (target >= 0) {
+        constexpr int U = 4;                                            // loads in flight
+        const int vecs = V / E::N;
+        const float c = a.r.c, c_lo = a.r.c_lo;
+        int v = threadIdx.x;
+        for (; v + (U - 1) * nt < vecs; v += U * nt) {
+            u32x4_any w[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(v + k * nt) * E::N);
+            float z[U][E::N], m = p.m;
+#pragma unroll
+            for (int k = 0; k < U; ++k) { E::unpack(w[k], z[k]); m = max_of(z[k], m); }
+            if (m > p.m) rescale<FINE>(p, m, c, c_lo);
+            const Shift s = shift_of(m, c);
+            const float m0 = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int k = 0; k < U; ++k) add_at<FINE>(p, z[k], m0, s, c, c_lo);
+        }
+        for (; v < vecs; v += nt) {
+            float z[E::N];
+            E::unpack(*reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N), z);
+            add_elements<FINE>(p, z, c, c_lo);
+        }
+        const int j = vecs * E::N + threadIdx.x;
+        if (j < V) {
+            const float z[1] = {E::get(row + j)};
+            add_elements<FINE>(p, z, c, c_lo);
+        }
+        p = block_joined<FINE>(p, c, c_lo, lds);
+    }
+    if (threadIdx.x == 0) store_sums<FINE>(a, n, p, target, target >= 0 ? E::get(row + target) : 0.0f);
+}
+
+// ---------------------------------------------------------------------------
+// d / d logits of a row, element by element, from its coefficients; bound by the read and the write.  Rows are taken from the
+// last to the first: after a pass of sums over the same logits the last ones may still lie in the last-level cache.
+// ---------------------------------------------------------------------------
+template <class E, bool ENT>
+__global__ __launch_bounds__(WG) void block_gradients(const GradArgs a)
+{
+    typedef typename E::T T;
+    __shared__ double lds[WG / 64];
+    if (a.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.fin, lds); return; }
+    const int64_t n = a.r.rows - 1 - blockIdx.x;
+    const RowGrad q = grad_of_row(a, n);
+    const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
+    T* out = static_cast<T*>(a.out) + n * a.out_stride;
+    const int V = a.r.V, vecs = V / E::N;
+    if (q.target < 0) {
+        for (int v = threadIdx.x; v < vecs; v += WG) *reinterpret_cast<u32x4_any*>(out + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
+        for (int j = vecs * E::N + threadIdx.x; j < V; j += WG) E::put(out + j, 0.0f);
+        return;
+    }
+    constexpr int U = 4;
+    int v = threadIdx.x;
+    const int tv = q.target / E::N;
+    auto piece = [&](int at, const u32x4_any& w) {
+        float z[E::N], d[E::N];
+        E::unpack(w, z);
+        gradient_of<ENT>(q, z, d);
+        if (at == tv) {
+#pragma unroll
+            for (int i = 0; i < E::N; ++i) d[i] += at * E::N + i == q.target ? q.to_target : 0.0f;
+        }
+        *reinterpret_cast<u32x4_any*>(out + (int64_t)at * E::N) = E::pack(d);
+    };
+    for (; v + (U - 1) * WG < vecs; v += U * WG) {
+        u32x4_any w[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(v + k * WG) * E::N);
+#pragma unroll
+        for (int k = 0; k < U; ++k) piece(v + k * WG, w[k]);
+    }
+    for (; v < vecs; v += WG) piece(v, *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N));
+    const int j = vecs * E::N + threadIdx.x;
+    if (j < V) {
+        float z[1] = {E::get(row + j)}, d[1];
+        gradient_of<ENT>(q, z, d);
+        E::put(out + j, d[0] + (j == q.target ? q.to_target : 0.0f));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The clipped loss over long rows: a workgroup of NT threads holds a row in registers, VPT pieces of 16 bytes a thread, from
+// the one read to the one write; of a row longer than that the rest is read again.
+// ---------------------------------------------------------------------------
+template <class E, int NT, int VPT, bool ENT>
+__global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
+{
+    typedef typename E::T T;
+    constexpr int WAVES = NT / 64;
+    __shared__ Part lds[WAVES];
+    __shared__ double weights[WAVES];
+    __shared__ RowGrad row_grad;
+    const int64_t n = blockIdx.x;
+    const int V = a.r.V, vecs = V / E::N, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int target = policy_target(a, n);
+    const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
+    T* out = static_cast<T*>(a.out) + n * a.out_stride;
+    if (target < 0) {
+        if (a.out) {
+            for (int v = tid; v < vecs; v += NT) *reinterpret_cast<u32x4_any*>(out + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
+            for (int j = vecs * E::N + tid; j < V; j += NT) E::put(out + j, 0.0f);
+        }
+        if (tid == 0) {
+            if (a.logp) a.logp[n] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < STATS; ++k) a.parts[n].v[k] = 0.0;
+        }
+        return;
+    }
+    u32x4_any w[VPT];
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+        if (tid + k * NT < vecs) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(tid + k * NT) * E::N);
+    const int j_tail = vecs * E::N + tid;
+    const float z_tail = j_tail < V ? E::get(row + j_tail) : -INFINITY;
+    const float chosen = E::get(row + target);
+    const double share = wave_sum(weight_share(a.norm, a.r, tid, NT));
+    // maximum of the wavefront's pieces, then their sums at that shift
+    const float c = a.r.c, c_lo = a.r.c_lo;
+    float m = z_tail;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+        if (tid + k * NT < vecs) { float z[E::N]; E::unpack(w[k], z); m = max_of(z, m); }
+    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    Part p{m, 0.0f, 0.0f};
+    const Shift s = shift_of(m, c);
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+        if (tid + k * NT < vecs) { float z[E::N]; E::unpack(w[k], z); add_at<false>(p, z, 0.0f, s, c, c_lo); }
+    if (j_tail < V) { const float z[1] = {z_tail}; add_at<false>(p, z, 0.0f, s, c, c_lo); }
+    for (int v = tid + VPT * NT; v < vecs; v += NT) {
+        float z[E::N];
+        E::unpack(*reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N), z);
+        add_elements<false>(p, z, c, c_lo);
+    }
+    p = lanes_joined<false>(p, c, c_lo, 64);
+    if (lane == 0) { lds[wave] = p; weights[wave] = share; }
+    __syncthreads();
+    if (wave == 0) {
+        p = lds[lane < WAVES ? lane : 0];
+        p = lanes_joined<false>(p, c, c_lo, WAVES);
+        const double W = wave_sum(lane < WAVES ? weights[lane] : 0.0);
+        if (lane == 0) {
+            const RowSum x = finish_row<false>(p, a.r);
+            const double lp = logp_of<false>(x, chosen, a.r), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
+            const PolicyRow y = policy_row(a.p, n, lp, x.entropy, x.empty);
+            row_grad = row_gradient(x, y.g * inv, y.e * inv, target, a.r.scale);
+            if (a.logp) a.logp[n] = (float)lp;
+            double v[STATS] = {};
+            add_stats(v, y);
+#pragma unroll
+            for (int k = 0; k < STATS; ++k) a.parts[n].v[k] = v[k];
+        }
+    }
+    if (!a.out) return;
+    __syncthreads();
+    const RowGrad q = row_grad;
+    const int tv = q.target / E::N;
+    auto piece = [&](int at, const u32x4_any& x) {
+        float z[E::N], d[E::N];
+        E::unpack(x, z);
+        gradient_of<ENT>(q, z, d);
+        if (at == tv) {
+#pragma unroll
+            for (int i = 0; i < E::N; ++i) d[i] += at * E::N + i == q.target ? q.to_target : 0.0f;
+        }
+        *reinterpret_cast<u32x4_any*>(out + (int64_t)at * E::N) = E::pack(d);
+    };
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+        if (tid + k * NT < vecs) piece(tid + k * NT, w[k]);
+    for (int v = tid + VPT * NT; v < vecs; v += NT) piece(v, *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N));
+    if (j_tail < V) {
+        float z[1] = {z_tail}, d[1];
+        gradient_of<ENT>(q, z, d);
+        E::put(out + j_tail, d[0] + (j_tail == q.target ? q.to_target : 0.0f));
+    }
 }
 
 // ---------------------------------------------------------------------------
 // A workgroup per pair: the summed log ratios of its two sequences, the loss of their difference h, and the coefficient
-// of every row:  dL/dlp = +- w beta ((1 - y) sigmoid(h) - y sigmoid(-h)) (/ tokens)  (without 1 / W).
+// of every row:  dL/dlp = +- w beta ((1 - y) sigmoid(h) - y sigmoid(-h)) (/ tokens)  (over W).
 // ---------------------------------------------------------------------------
 struct PairArgs {
+    Rows r;
     Seqs q;
     const RowWs* ws;
     const float *ref, *label, *weight;
@@ -297,7 +570,7 @@ __global__ __launch_bounds__(WG) void pair_sums(const PairArgs a)
 {
     __shared__ double lds[WG / 64];
     const int64_t P = a.q.count / 2;
-    const double W = weight_total(a.norm), inv = W != 0.0 ? a.grad_scale / W : 0.0;
+    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, WG), lds), inv = W != 0.0 ? a.grad_scale / W : 0.0;
     double v[STATS] = {};
     for (int64_t k = blockIdx.x; k < P; k += gridDim.x) {
         const Seq s[2] = {sequence(a.q, k), sequence(a.q, k + P)};
@@ -347,18 +620,22 @@ int32_t fail_hip(hipError_t e)
 }
 static int type_bytes(int type) { return type == ANAKIN_TYPE_FP32 ? 4 : 2; }
 
-constexpr int MAX_PARTS = 1024;                  // workgroups that report sums at most
+struct LaneForm { int lanes; int pieces; };       // pieces 0: single elements; lanes 0: longer than that
+static LaneForm lane_form(int type, int64_t V);
+constexpr int MAX_PARTS = 2048;                   // workgroups of short rows (8 for every compute unit) and of pairs that report sums at most
 
-struct RowsWs { size_t ws, to_logp, to_entropy, weights, parts, total; };
-static RowsWs rows_workspace(int64_t rows)
+// log-probabilities need none; the clipped loss room for the weights' and the workgroups' sums; pairs rows of their own too
+struct RowsWs { size_t weights, parts, ws, to_logp, total; };
+static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
 {
     RowsWs w;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
-    w.ws = take((size_t)rows * sizeof(RowWs));
-    w.to_logp = take((size_t)rows * 4); w.to_entropy = take((size_t)rows * 4);
     w.weights = take(WEIGHT_PARTS * sizeof(double));
-    w.parts = take(MAX_PARTS * sizeof(Partial));
+    const bool lanes = lane_form(ANAKIN_TYPE_FP32, vocab).lanes > 0;    // (fp32 rows are the first to take workgroups)
+    w.parts = take((size_t)(!lanes && rows > MAX_PARTS ? rows : MAX_PARTS) * sizeof(Partial));
+    w.ws = take(pairs ? (size_t)rows * sizeof(RowWs) : 0);
+    w.to_logp = take(pairs ? (size_t)rows * 4 : 0);
     w.total = off;
     return w;
 }
@@ -380,7 +657,7 @@ static int32_t check_rows(const anakin_rows* x, Rows& r)
     r.logits = x->d_logits; r.target = x->d_target; r.rows = x->rows; r.stride = x->row_stride; r.V = (int)x->vocab;
     r.target_type = x->target_type; r.scale = x->scale;
     const double c = x->scale * LOG2E;
-    r.c = (float)c; r.dc = c - (double)r.c;
+    r.c = (float)c; r.dc = c - (double)r.c; r.c_lo = (float)r.dc; r.inv_c = 1.0 / (double)r.c;
     return ANAKIN_OK;
 }
 static int32_t check_gradient(const anakin_rows* x, const void* out, int64_t stride)
@@ -409,30 +686,97 @@ int32_t check_workspace(const void* ws, size_t have, size_t need)
 }
 static bool is_finite(double x) { return x - x == 0.0; }
 
-static unsigned row_grid(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
-static unsigned part_grid(int64_t n, int64_t per) { const int64_t g = (n + per - 1) / per; return (unsigned)(g < 1 ? 1 : g > MAX_PARTS ? MAX_PARTS : g); }
+// ---- which form a row takes ----------------------------------------------------------------------------------------
+// Lanes: the fewest (a power of two) that hold a row with 4 single elements each, up to 64 lanes and 256 columns; then
+// wavefronts with 1 or 4 pieces of 16 bytes a lane.  Longer rows take a workgroup.
+static LaneForm lane_form(int type, int64_t V)
+{
+    const int64_t per = type == ANAKIN_TYPE_FP32 ? 4 : 8;
+    if (V <= 256) { int l = 1; while (l * 4 < V) l *= 2; return LaneForm{l, 0}; }
+    if (V <= 64 * per) return LaneForm{64, 1};
+    if (V <= 256 * per) return LaneForm{64, 4};
+    return LaneForm{0, 0};
+}
+static unsigned lane_grid(const LaneForm& f, int64_t rows)
+{
+    const int64_t per = WG / f.lanes, g = (rows + per - 1) / per;
+    return (unsigned)(g < 1 ? 1 : g > MAX_PARTS ? MAX_PARTS : g);
+}
+template <class E, int DO, bool FINE>
+static void launch_lanes(const LaneForm& f, const LaneArgs& a, unsigned grid, hipStream_t s)
+{
+    auto k = f.pieces == 0 ? lanes_rows<E, DO, 4, false, FINE> : f.pieces == 1 ? lanes_rows<E, DO, E::N, true, FINE> : lanes_rows<E, DO, 4 * E::N, true, FINE>;
+    hipLaunchKernelGGL(k, dim3(grid), dim3(WG), 0, s, a);
+}
+#define BY_TYPE(type, f, ...) ((type) == ANAKIN_TYPE_FP32 ? f<Fp32, __VA_ARGS__> : (type) == ANAKIN_TYPE_BF16 ? f<Bf16, __VA_ARGS__> : f<Fp16, __VA_ARGS__>)
 
-static hipError_t launch_row_sums(int type, const SumArgs& a, hipStream_t s)
+static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t s)
 {
     if (a.r.rows == 0) return hipSuccess;
-    auto k = type == ANAKIN_TYPE_FP32 ? row_sums<Fp32> : type == ANAKIN_TYPE_BF16 ? row_sums<Bf16> : row_sums<Fp16>;
-    hipLaunchKernelGGL(k, dim3(row_grid(a.r.rows)), dim3(WG), 0, s, a);
+    const LaneForm f = lane_form(type, a.r.V);
+    if (f.lanes) {
+        LaneArgs l{};
+        l.lanes = f.lanes; l.s = a;
+        if (fine) BY_TYPE(type, launch_lanes, DO_SUMS, true)(f, l, lane_grid(f, a.r.rows), s);
+        else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
+    } else {
+        // few rows: as many threads to a row as there are
+        const dim3 block(a.r.rows <= 512 ? 1024 : 256);
+        if (fine) hipLaunchKernelGGL(BY_TYPE(type, block_sums, true), dim3((unsigned)a.r.rows), block, 0, s, a);
+        else hipLaunchKernelGGL(BY_TYPE(type, block_sums, false), dim3((unsigned)a.r.rows), block, 0, s, a);
+    }
     return hipGetLastError();
 }
-static hipError_t launch_row_gradients(int type, const GradArgs& a, bool ent, hipStream_t s)
+static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStream_t s)
 {
-    if (a.r.rows == 0) return hipSuccess;
-    auto k = ent ? (type == ANAKIN_TYPE_FP32 ? row_gradients<Fp32, true> : type == ANAKIN_TYPE_BF16 ? row_gradients<Bf16, true> : row_gradients<Fp16, true>)
-                 : (type == ANAKIN_TYPE_FP32 ? row_gradients<Fp32, false> : type == ANAKIN_TYPE_BF16 ? row_gradients<Bf16, false> : row_gradients<Fp16, false>);
-    hipLaunchKernelGGL(k, dim3(row_grid(a.r.rows)), dim3(WG), 0, s, a);
+    const unsigned more = a.fin.stats ? 1 : 0;
+    const LaneForm f = lane_form(type, a.r.V);
+    if (a.r.rows == 0 && !more) return hipSuccess;
+    if (f.lanes) {
+        LaneArgs l{};
+        l.lanes = f.lanes; l.g = a;
+        BY_TYPE(type, launch_lanes, DO_GRADIENT, false)(f, l, lane_grid(f, a.r.rows) + more, s);
+    } else if (ent) hipLaunchKernelGGL(BY_TYPE(type, block_gradients, true), dim3((unsigned)a.r.rows + more), dim3(WG), 0, s, a);
+    else hipLaunchKernelGGL(BY_TYPE(type, block_gradients, false), dim3((unsigned)a.r.rows + more), dim3(WG), 0, s, a);
     return hipGetLastError();
 }
-// W: the given norm, or partial sums of the weights (of rows, or of `pairs` pairs)
+template <class E, bool ENT>
+static void launch_block_policy(const PolicyArgs& a, hipStream_t s)
+{
+    // the smallest workgroup whose registers hold a row; beyond 1024 threads of 16 pieces the rest is read twice
+    const int64_t pieces = (a.r.V + E::N - 1) / E::N;
+    const dim3 grid((unsigned)a.r.rows);
+    if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, ENT>), grid, dim3(256), 0, s, a);
+    else if (pieces <= 1024 * 4) hipLaunchKernelGGL((block_policy<E, 1024, 4, ENT>), grid, dim3(1024), 0, s, a);
+    else if (pieces <= 1024 * 8) hipLaunchKernelGGL((block_policy<E, 1024, 8, ENT>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((block_policy<E, 1024, 16, ENT>), grid, dim3(1024), 0, s, a);
+}
+// *parts: how many workgroups report sums
+static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipStream_t s)
+{
+    *parts = 0;
+    if (a.r.rows == 0) return hipSuccess;
+    const LaneForm f = lane_form(type, a.r.V);
+    if (f.lanes) {
+        LaneArgs l{};
+        l.lanes = f.lanes; l.p = a;
+        const unsigned grid = lane_grid(f, a.r.rows);
+        *parts = (int)grid;
+        BY_TYPE(type, launch_lanes, DO_POLICY, false)(f, l, grid, s);
+    } else {
+        *parts = (int)a.r.rows;
+        if (a.p.ent != 0.0) BY_TYPE(type, launch_block_policy, true)(a, s);
+        else BY_TYPE(type, launch_block_policy, false)(a, s);
+    }
+    return hipGetLastError();
+}
+// W: the given norm, the rows' own weights where they are few, or partial sums (of rows', or of `pairs` pairs' weights)
 static hipError_t launch_weights(const Rows& r, int64_t n, const float* weight, bool pairs, double norm, double* parts, Norm& w, hipStream_t s)
 {
-    w.norm = norm; w.parts = parts; w.n_parts = 0;
+    w = Norm{norm, parts, 0, weight, 0};
     if (norm != 0.0 || n == 0) return hipSuccess;
     if (pairs && !weight) { w.norm = (double)n; return hipSuccess; }
+    if (!pairs && n <= INLINE_ROWS) { w.inline_rows = (int)n; return hipSuccess; }
     const int64_t g = (n + 4 * WG - 1) / (4 * WG);
     w.n_parts = (int)(g > WEIGHT_PARTS ? WEIGHT_PARTS : g);
     hipLaunchKernelGGL(weight_sums, dim3(w.n_parts), dim3(WG), 0, s, r, n, weight, pairs, parts);
@@ -449,7 +793,7 @@ using namespace ank;
 extern "C" size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64_t pairs)
 {
     if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > MAX_VOCAB || pairs < 0 || pairs > MAX_ROWS) return 0;
-    return rows_workspace(rows).total;
+    return rows_workspace(rows, vocab, pairs).total;
 }
 
 extern "C" int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy,
@@ -458,9 +802,9 @@ extern "C" int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, fl
     SumArgs a{};
     TRY(check_rows(x, a.r));
     if (x->rows > 0 && (!d_logp || !d_lse)) return fail(ANAKIN_E_INVALID_ARG, "null logp or lse");
-    TRY(check_workspace(d_workspace, workspace_bytes, rows_workspace(x->rows).total));
+    TRY(check_workspace(d_workspace, workspace_bytes, rows_workspace(x->rows, x->vocab, 0).total));
     a.logp = d_logp; a.lse = d_lse; a.entropy = d_entropy;
-    LAUNCH(launch_row_sums(x->type, a, static_cast<hipStream_t>(hip_stream)));
+    LAUNCH(launch_sums(x->type, a, false, static_cast<hipStream_t>(hip_stream)));
     return ANAKIN_OK;
 }
 
@@ -474,7 +818,7 @@ extern "C" int32_t anakin_token_logprobs_backward(const anakin_rows* x, const fl
     if (d_grad_entropy && !d_entropy) return fail(ANAKIN_E_INVALID_ARG, "grad_entropy needs the entropy of the forward call");
     TRY(check_gradient(x, d_dlogits, grad_stride));
     a.out = d_dlogits; a.out_stride = grad_stride; a.lse = d_lse; a.entropy = d_entropy; a.to_logp = d_grad_logp; a.to_entropy = d_grad_entropy;
-    LAUNCH(launch_row_gradients(x->type, a, d_grad_entropy != nullptr, static_cast<hipStream_t>(hip_stream)));
+    LAUNCH(launch_gradients(x->type, a, d_grad_entropy != nullptr, static_cast<hipStream_t>(hip_stream)));
     return ANAKIN_OK;
 }
 
@@ -491,30 +835,22 @@ extern "C" int32_t anakin_policy_loss(const anakin_rows* x, const anakin_policy_
         return fail(ANAKIN_E_INVALID_ARG, "a coefficient is not finite, or norm is negative");
     if (a->kl_coef != 0.0 && !a->d_logp_ref && x->rows > 0) return fail(ANAKIN_E_INVALID_ARG, "kl_coef needs logp_ref");
     if (a->d_dlogits) TRY(check_gradient(x, a->d_dlogits, a->grad_stride));
-    const RowsWs w = rows_workspace(x->rows);
+    const RowsWs w = rows_workspace(x->rows, x->vocab, 0);
     TRY(check_workspace(d_workspace, workspace_bytes, w.total));
     char* base = static_cast<char*>(d_workspace);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     PolicyArgs p{};
-    p.p = PolicyCfg{a->d_logp_old, a->d_adv, a->d_logp_ref, a->d_weight, a->clip_low, a->clip_high, a->kl_coef, a->entropy_coef, a->grad_scale};
-    p.rows = x->rows; p.ws = reinterpret_cast<RowWs*>(base + w.ws);
-    p.to_logp = reinterpret_cast<float*>(base + w.to_logp); p.to_entropy = reinterpret_cast<float*>(base + w.to_entropy);
+    p.r = r;
+    p.p = PolicyCfg{a->d_logp_old, a->d_adv, a->d_logp_ref, a->d_weight, log1p(-a->clip_low), log1p(a->clip_high), 1.0 - a->clip_low, 1.0 + a->clip_high,
+                    a->kl_coef, a->entropy_coef, a->grad_scale};
+    p.logp = a->d_logp; p.out = a->d_dlogits; p.out_stride = a->grad_stride;
     p.parts = reinterpret_cast<Partial*>(base + w.parts);
     LAUNCH(launch_weights(r, x->rows, a->d_weight, false, a->norm, reinterpret_cast<double*>(base + w.weights), p.norm, s));
-    SumArgs sum{};
-    sum.r = r; sum.weight = a->d_weight; sum.logp = a->d_logp; sum.ws = reinterpret_cast<RowWs*>(base + w.ws);
-    LAUNCH(launch_row_sums(x->type, sum, s));
-    const unsigned blocks = part_grid(x->rows, WG);
-    hipLaunchKernelGGL(policy_rows, dim3(blocks), dim3(WG), 0, s, p);
+    int parts = 0;
+    LAUNCH(launch_policy(x->type, p, &parts, s));
+    const FinishArgs f{p.parts, parts, r, p.norm, a->d_stats, a->kl_coef, a->entropy_coef, 1};
+    hipLaunchKernelGGL(finish_stats, dim3(1), dim3(parts > 64 ? FINISH_WG : 64), 0, s, f);
     LAUNCH(hipGetLastError());
-    const FinishArgs f{p.parts, (int)blocks, p.norm, a->d_stats, a->kl_coef, a->entropy_coef, 1};
-    hipLaunchKernelGGL(finish_stats, dim3(1), dim3(WG), 0, s, f);
-    LAUNCH(hipGetLastError());
-    if (a->d_dlogits) {
-        GradArgs g{};
-        g.r = r; g.out = a->d_dlogits; g.out_stride = a->grad_stride; g.ws = p.ws; g.to_logp = p.to_logp; g.to_entropy = p.to_entropy;
-        LAUNCH(launch_row_gradients(x->type, g, a->entropy_coef != 0.0, s));
-    }
     return ANAKIN_OK;
 }
 
@@ -544,12 +880,13 @@ extern "C" int32_t anakin_preference_loss(const anakin_rows* x, const anakin_seq
     if (!is_finite(a->beta) || !is_finite(a->margin) || !is_finite(a->grad_scale) || !is_finite(a->norm) || a->norm < 0.0)
         return fail(ANAKIN_E_INVALID_ARG, "a coefficient is not finite, or norm is negative");
     if (a->d_dlogits) TRY(check_gradient(x, a->d_dlogits, a->grad_stride));
-    const RowsWs w = rows_workspace(x->rows);
+    const int64_t P = q->count / 2;
+    const RowsWs w = rows_workspace(x->rows, x->vocab, P > 0 ? P : 1);
     TRY(check_workspace(d_workspace, workspace_bytes, w.total));
     char* base = static_cast<char*>(d_workspace);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const int64_t P = q->count / 2;
     PairArgs p{};
+    p.r = r;
     p.q = Seqs{q->layout, q->count, q->length, x->rows, q->d_offsets, q->d_lengths};
     p.ws = reinterpret_cast<RowWs*>(base + w.ws);
     p.ref = a->d_logp_ref; p.label = a->d_label; p.weight = a->d_weight; p.beta = a->beta; p.margin = a->margin; p.grad_scale = a->grad_scale;
@@ -557,17 +894,19 @@ extern "C" int32_t anakin_preference_loss(const anakin_rows* x, const anakin_seq
     LAUNCH(launch_weights(r, P, a->d_weight, true, a->norm, reinterpret_cast<double*>(base + w.weights), p.norm, s));
     SumArgs sum{};
     sum.r = r; sum.logp = a->d_logp; sum.ws = reinterpret_cast<RowWs*>(base + w.ws); sum.coef = p.to_logp;
-    LAUNCH(launch_row_sums(x->type, sum, s));
-    const unsigned blocks = part_grid(P, 1);
+    LAUNCH(launch_sums(x->type, sum, true, s));
+    const unsigned blocks = (unsigned)(P < 1 ? 1 : P > MAX_PARTS ? MAX_PARTS : P);
     hipLaunchKernelGGL(pair_sums, dim3(blocks), dim3(WG), 0, s, p);
     LAUNCH(hipGetLastError());
-    const FinishArgs f{p.parts, (int)blocks, p.norm, a->d_stats, 0.0, 0.0, 0};
-    hipLaunchKernelGGL(finish_stats, dim3(1), dim3(WG), 0, s, f);
-    LAUNCH(hipGetLastError());
-    if (a->d_dlogits) {
+    const FinishArgs f{p.parts, (int)blocks, r, p.norm, a->d_stats, 0.0, 0.0, 0};
+    if (a->d_dlogits && x->rows > 0) {
+        // the gradient's launch finishes the statistics too
         GradArgs g{};
-        g.r = r; g.out = a->d_dlogits; g.out_stride = a->grad_stride; g.ws = p.ws; g.to_logp = p.to_logp;
-        LAUNCH(launch_row_gradients(x->type, g, false, s));
+        g.r = r; g.out = a->d_dlogits; g.out_stride = a->grad_stride; g.ws = p.ws; g.to_logp = p.to_logp; g.fin = f;
+        LAUNCH(launch_gradients(x->type, g, false, s));
+    } else {
+        hipLaunchKernelGGL(finish_stats, dim3(1), dim3(blocks > 64 ? FINISH_WG : 64), 0, s, f);
+        LAUNCH(hipGetLastError());
     }
     return ANAKIN_OK;
 }

@@ -201,7 +201,7 @@ def preference_loss(logits, target, sequences, *, beta=0.1, margin=0.0, mean=Fal
     out, stride = c.gradient(logits, out) if gradient else (None, 0)
     a = binding.PreferenceArgs(c.vector(logp_ref, n, "logp_ref"), c.vector(label, pairs, "label"), c.vector(weight, pairs, "weight"), beta, margin, norm,
                                grad_scale, 1 if mean else 0, stats.data_ptr(), margins.data_ptr(), logp.data_ptr(), out.data_ptr() if gradient else None, stride)
-    ws = c.empty(c.L.anakin_rows_workspace_bytes(n, x.vocab, pairs), torch.uint8)
+    ws = c.empty(c.L.anakin_rows_workspace_bytes(n, x.vocab, max(1, pairs)), torch.uint8)
     c.run(c.L.anakin_preference_loss, x, q, a, ws.data_ptr(), ws.numel())
     return PreferenceLoss(stats, margins, logp, out)
 
