@@ -307,8 +307,8 @@ int32_t anakin_peak_probe(int32_t kind, int32_t workgroups, void* scratch, size_
  * The losses and targets above are tied to a handle's own few head outputs.  These calls take them to any policy that
  * picks one of `vocab` choices per row of a matrix of logits (a row being a token of a sequence, or a sample of an
  * unroll): log-probabilities, a clipped policy loss, a loss over pairs of sequences, and returns over sequences of
- * unequal length.  No handle: the caller passes device pointers, a workspace (256-byte aligned, of the size the
- * matching *_workspace_bytes returns) and a stream of the device that holds them, which has to be the current device;
+ * unequal length.  No handle: the caller passes device pointers, a workspace where the call has one (256-byte
+ * aligned, of the size the matching *_workspace_bytes returns) and a stream of the device that holds them, which has to be the current device;
  * everything is enqueued on that stream, nothing synchronises, and nothing is kept between calls.  Two calls that may
  * overlap in time need workspaces of their own.  Calls can be captured into a HIP graph.  Errors are found on the host
  * before anything is enqueued; anakin_last_error(NULL) has the message (per thread).  Results do not depend on
@@ -328,15 +328,10 @@ typedef struct {
     double scale;
 } anakin_rows;
 
-/* Workspace of the calls that take an anakin_rows; pairs: count / 2 for the preference loss, 1 at least, and 0 for the
- * other calls.  Returns 0 for sizes out of range. */
-size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64_t pairs);
-
 /* logp[n] = log softmax(scale * logits[n])[target[n]], lse[n] = log sum exp(scale * logits[n]), and (where not null)
  * entropy[n] = -sum p log p.  Rows that take no part get zeros; a row all of whose logits are minus infinity gets
  * logp = lse = -inf and entropy 0. */
-int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy,
-                              void* d_workspace, size_t workspace_bytes, void* hip_stream);
+int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy, void* hip_stream);
 
 /* Its backward pass: dlogits[n][j] = scale (g[n] ([j = target[n]] - p_j) - e[n] p_j (log p_j + entropy[n])) with
  * g = d_grad_logp, e = d_grad_entropy (null: 0; else d_entropy has to be given) and p from the lse of the forward call.
@@ -345,6 +340,10 @@ int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse,
 int32_t anakin_token_logprobs_backward(const anakin_rows* x, const float* d_lse, const float* d_entropy,
                                        const float* d_grad_logp, const float* d_grad_entropy,
                                        void* d_dlogits, int64_t grad_stride, void* hip_stream);
+
+/* Workspace of the two losses below; pairs: count / 2 for the preference loss, 1 at least, and 0 for the policy loss.
+ * Returns 0 for sizes out of range. */
+size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64_t pairs);
 
 /* Clipped policy loss with a KL term and an entropy bonus, and its gradient, in one call.  With lp = log pi(target) and
  * r = exp(lp - logp_old):  l = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - d - 1) - entropy_coef H,

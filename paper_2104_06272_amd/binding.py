@@ -149,7 +149,7 @@ def load():
     i64, sz, rows, seq = C.c_int64, C.c_size_t, C.POINTER(Rows), C.POINTER(SequenceArgs)
     L.anakin_rows_workspace_bytes.argtypes = [i64, i64, i64]
     L.anakin_returns_workspace_bytes.argtypes = [i64, i64]
-    L.anakin_token_logprobs.argtypes = [rows, vp, vp, vp, vp, sz, vp]
+    L.anakin_token_logprobs.argtypes = [rows, vp, vp, vp, vp]
     L.anakin_token_logprobs_backward.argtypes = [rows, vp, vp, vp, vp, vp, i64, vp]
     L.anakin_policy_loss.argtypes = [rows, C.POINTER(PolicyArgs), vp, sz, vp]
     L.anakin_preference_loss.argtypes = [rows, seq, C.POINTER(PreferenceArgs), vp, sz, vp]

@@ -134,22 +134,29 @@ __device__ __forceinline__ Part joined(Part a, Part b, float c, float c_lo)
     rescale<FINE>(a, m, c, c_lo); rescale<FINE>(b, m, c, c_lo);
     return Part{m, a.s + b.s, a.u + b.u};
 }
-// elements at shift k (coarse) or maximum m (fine)
+// elements at shift k (coarse) or maximum m (fine); s grows by their sum, which is a tree: a thread of a long row adds a few
+// dozen times and not a few hundred
 template <bool FINE, int N>
 __device__ __forceinline__ void add_at(Part& p, const float (&z)[N], float m, const Shift& k, float c, float c_lo)
 {
+    float e[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if (FINE) {
-            const float x = z[i] - m, t = x * c, e = __builtin_amdgcn_exp2f(t);
-            p.s += e;
-            p.u = fmaf(e, __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -t)), -1.0f, 1.0f), p.u);
+            const float x = z[i] - m, t = x * c;
+            e[i] = __builtin_amdgcn_exp2f(t);
+            p.u = fmaf(e[i], __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -t)), -1.0f, 1.0f), p.u);
         } else {
-            const float t = fmaf(z[i], k.c, -k.K), e = __builtin_amdgcn_exp2f(t);
-            p.s += e;
-            p.u = fmaf(e, fmaxf(t, T_MIN), p.u);
+            const float t = fmaf(z[i], k.c, -k.K);
+            e[i] = __builtin_amdgcn_exp2f(t);
+            p.u = fmaf(e[i], fmaxf(t, T_MIN), p.u);
         }
     }
+#pragma unroll
+    for (int w = 1; w < N; w *= 2)
+#pragma unroll
+        for (int i = 0; i + w < N; i += 2 * w) e[i] += e[i + w];
+    p.s += e[0];
 }
 template <int N>
 __device__ __forceinline__ float max_of(const float (&z)[N], float m)   // (passes over a NaN)
@@ -203,6 +210,10 @@ __device__ __forceinline__ float exp_of(double x)
     return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(t - i)), (int)i);
 }
 
+// A row's sums as its workgroup or its lanes have them together: `fine` ones are joined in 64 bits, since the roundings of
+// the last few additions in 32 would be most of what is left (u is in s then).
+struct Sums { float m; double s, u; };
+
 struct RowSum {
     double lse, entropy, log_s;                  // log_s: with the shift's own c
     float m; Shift k;
@@ -210,22 +221,22 @@ struct RowSum {
     bool far, empty;                             // empty: all of it minus infinity
 };
 template <bool FINE>
-__device__ __forceinline__ RowSum finish_row(const Part& p, const Rows& r)
+__device__ __forceinline__ RowSum finish_row(const Sums& p, const Rows& r)
 {
     RowSum x{};
+    const double s = p.s;
     x.m = p.m; x.far = is_far(p.m, r.c);
-    x.empty = p.m == -INFINITY && p.s == 0.0f;
+    x.empty = p.m == -INFINITY && s == 0.0;
     x.k = shift_of(p.m, r.c);
     if (x.empty) { x.lse = -INFINITY; return x; }
     if (FINE) {
-        const double s = fma(LN2, (double)p.u, (double)p.s);
         x.log_s = log_of_sum(s);
         x.lse = fma(r.scale, (double)p.m, x.log_s);
         // the shift of the gradient: 2^(c z - K) / s' with K = fl(c m)
         x.inv_s = (float)(reciprocal(s) * (x.far ? 1.0 : (double)exp_of(((double)x.k.K - (double)r.c * (double)p.m) * LN2)));
         return x;
     }
-    const double s = (double)p.s, inv = reciprocal(s), mean_t = (double)p.u * inv;      // E[t]
+    const double inv = reciprocal(s), mean_t = p.u * inv;               // E[t]
     x.log_s = log_of_sum(s);
     // c stands for scale log2 e (off by 2^-25 of it): to first order that adds  ln 2 (exact c - c) E[z]  to the log-sum-exp
     if (x.far) x.lse = fma(r.scale, (double)p.m, x.log_s);

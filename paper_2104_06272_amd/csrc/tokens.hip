@@ -32,13 +32,34 @@ __device__ __forceinline__ double block_sum(double v, double* lds)      // every
     for (int w = 0; w < waves; ++w) s += lds[w];
     return s;
 }
-__device__ __forceinline__ void block_partial(const double (&v)[STATS], double* lds, Partial* out)
+// Eight sums at once: in three steps every lane gives half of what it holds to its partner and adds what it is given, in three
+// more the lanes of one sum join.  The lane's sum is number stat_of(lane).
+__device__ __forceinline__ int stat_of(int lane) { return ((lane >> 5) & 1) * 4 + ((lane >> 4) & 1) * 2 + ((lane >> 3) & 1); }
+__device__ __forceinline__ double wave_stats(const double (&v)[STATS])
 {
-    double s[STATS];
+    const int lane = threadIdx.x & 63;
+    double w[4], x[2];
 #pragma unroll
-    for (int k = 0; k < STATS; ++k) s[k] = block_sum(v[k], lds);
-    if (threadIdx.x == 0)
-        for (int k = 0; k < STATS; ++k) out->v[k] = s[k];
+    for (int i = 0; i < 4; ++i) w[i] = (lane & 32 ? v[4 + i] : v[i]) + __shfl_xor(lane & 32 ? v[i] : v[4 + i], 32, 64);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = (lane & 16 ? w[2 + i] : w[i]) + __shfl_xor(lane & 16 ? w[i] : w[2 + i], 16, 64);
+    double y = (lane & 8 ? x[1] : x[0]) + __shfl_xor(lane & 8 ? x[0] : x[1], 8, 64);
+    for (int off = 4; off > 0; off >>= 1) y += __shfl_xor(y, off, 64);
+    return y;
+}
+// the workgroup's eight sums in `out` (LDS): y is this lane's share of sum k, and lanes `first` speak for theirs
+__device__ __forceinline__ void block_stats(double y, int k, bool first, double (*lds)[STATS], double (&out)[STATS])
+{
+    const int waves = blockDim.x >> 6;
+    __syncthreads();
+    if (first) lds[threadIdx.x >> 6][k] = y;
+    __syncthreads();
+    if (threadIdx.x < STATS) {
+        double s = 0.0;
+        for (int w = 0; w < waves; ++w) s += lds[w][threadIdx.x];
+        out[threadIdx.x] = s;
+    }
+    __syncthreads();
 }
 
 // What a mean is taken over: the given norm, or the sum of the weights -- of parts that weight_sums left, or of the rows
@@ -52,6 +73,7 @@ __device__ __forceinline__ double weight_share(const Norm& w, const Rows& r, int
     if (w.norm != 0.0) return thread == 0 ? w.norm : 0.0;
     double s = 0.0;
     for (int i = thread; i < w.n_parts; i += threads) s += w.parts[i];
+#pragma unroll 4
     for (int i = thread; i < w.inline_rows; i += threads) s += weight_of(r, w.weight, i);
     return s;
 }
@@ -61,6 +83,7 @@ __global__ __launch_bounds__(WG) void weight_sums(const Rows r, const int64_t n,
 {
     __shared__ double lds[WG / 64];
     double s = 0.0;
+#pragma unroll 4
     for (int64_t i = (int64_t)blockIdx.x * WG + threadIdx.x; i < n; i += (int64_t)gridDim.x * WG)
         s += pairs ? (double)weight[i] : weight_of(r, weight, i);
     s = block_sum(s, lds);
@@ -69,30 +92,48 @@ __global__ __launch_bounds__(WG) void weight_sums(const Rows r, const int64_t n,
 
 // means over W of the summed statistics; slot 0 becomes the loss
 struct FinishArgs { const Partial* parts; int n_parts; Rows r; Norm norm; float* stats; double kl, ent; int policy; };
-__device__ __forceinline__ void finish(const FinishArgs& a, double* lds)
+struct FinishLds { double waves[16][STATS], sums[STATS], weights[16]; };
+__device__ __forceinline__ void finish(const FinishArgs& a, FinishLds& lds)
 {
-    double v[STATS] = {};
-    for (int i = threadIdx.x; i < a.n_parts; i += blockDim.x)
-#pragma unroll
-        for (int k = 0; k < STATS; ++k) v[k] += a.parts[i].v[k];
-#pragma unroll
-    for (int k = 0; k < STATS; ++k) v[k] = block_sum(v[k], lds);
-    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, blockDim.x), lds), inv = W != 0.0 ? 1.0 / W : 0.0;
-    if (threadIdx.x != 0) return;
-    double m[STATS];
-#pragma unroll
-    for (int k = 0; k < STATS; ++k) m[k] = W != 0.0 ? v[k] * inv : 0.0;
-    if (a.policy) m[0] = m[1] + (a.kl != 0.0 ? a.kl * m[2] : 0.0) - (a.ent != 0.0 ? a.ent * m[3] : 0.0);
-    m[5] = a.policy ? m[5] : W;                                         // pairs: loss, [h > 0], first, second, h, W, pairs, tokens
-    m[6] = a.policy ? W : v[6];
-    m[7] = v[7];
-#pragma unroll
-    for (int k = 0; k < STATS; ++k) a.stats[k] = (float)m[k];
+    // lane l adds sum l % 8 of partials l / 8, l / 8 + threads / 8, ...: whole cache lines
+    const int k = threadIdx.x & 7;
+    double y = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x >> 3; i < a.n_parts; i += blockDim.x >> 3) y += a.parts[i].v[k];
+    for (int off = 8; off < 64; off <<= 1) y += __shfl_xor(y, off, 64);
+    const double share = weight_share(a.norm, a.r, threadIdx.x, blockDim.x);
+    block_stats(y, k, (threadIdx.x & 63) < STATS, lds.waves, lds.sums);
+    const double W = block_sum(share, lds.weights), inv = W != 0.0 ? reciprocal(W) : 0.0;
+    if (threadIdx.x >= STATS) return;
+    const double* v = lds.sums;
+    double m = W != 0.0 ? v[k] * inv : 0.0;
+    if (a.policy) {
+        if (k == 0) m = W != 0.0 ? (v[1] + (a.kl != 0.0 ? a.kl * v[2] : 0.0) - (a.ent != 0.0 ? a.ent * v[3] : 0.0)) * inv : 0.0;
+        if (k == 6) m = W;
+    } else {                                                            // loss, [h > 0], first, second, h, W, pairs, tokens
+        if (k == 5) m = W;
+        if (k == 6) m = v[6];
+    }
+    if (k == 7) m = v[7];
+    a.stats[k] = (float)m;
 }
-constexpr int FINISH_WG = 1024;
+// many partial sums (one of every long row): FOLDED workgroups make as many of them
+constexpr int FOLDED = 64, FOLD_FROM = 512;
+__global__ __launch_bounds__(WG) void fold_stats(const Partial* parts, const int n, Partial* out)
+{
+    __shared__ FinishLds lds;
+    const int k = threadIdx.x & 7;
+    double y = 0.0;
+#pragma unroll 4
+    for (int i = blockIdx.x * (WG / 8) + (threadIdx.x >> 3); i < n; i += FOLDED * (WG / 8)) y += parts[i].v[k];
+    for (int off = 8; off < 64; off <<= 1) y += __shfl_xor(y, off, 64);
+    block_stats(y, k, (threadIdx.x & 63) < STATS, lds.waves, lds.sums);
+    if (threadIdx.x < STATS) out[blockIdx.x].v[k] = lds.sums[k];
+}
+constexpr int FINISH_WG = 512;
 __global__ __launch_bounds__(FINISH_WG) void finish_stats(const FinishArgs a)
 {
-    __shared__ double lds[FINISH_WG / 64];
+    __shared__ FinishLds lds;
     finish(a, lds);
 }
 
@@ -107,7 +148,7 @@ struct SumArgs {
     float* coef;                                 // may be null: set to 0 (pair_sums fills in the rows of its sequences)
 };
 template <bool FINE>
-__device__ __forceinline__ void store_sums(const SumArgs& a, int64_t n, const Part& p, int target, float chosen)
+__device__ __forceinline__ void store_sums(const SumArgs& a, int64_t n, const Sums& p, int target, float chosen)
 {
     RowSum x{};
     double lp = 0.0;
@@ -165,20 +206,25 @@ struct PolicyCfg {
     double log_low, log_high;                    // ln(1 - clip_low), ln(1 + clip_high)
     double low, high, kl, ent, grad_scale;       // low = 1 - clip_low, high = 1 + clip_high
 };
+struct PolicyIn { float old, adv, ref, w; };      // what a row's loss reads, asked for before its logits
+__device__ __forceinline__ PolicyIn policy_in(const PolicyCfg& a, int64_t n)
+{
+    return PolicyIn{a.old[n], a.adv[n], a.ref ? a.ref[n] : 0.0f, a.weight ? a.weight[n] : 1.0f};
+}
 struct PolicyRow { double g, e, policy, kl, entropy, clipped, ratio, w; };
-__device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, int64_t n, double lp, double entropy, bool empty)
+__device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, const PolicyIn& in, double lp, double entropy, bool empty)
 {
     PolicyRow x{};
-    x.w = a.weight ? (double)a.weight[n] : 1.0;
+    x.w = (double)in.w;
     if (empty) return x;
-    const double A = a.adv[n], diff = lp - (double)a.old[n], r = (double)exp_of(diff);
+    const double A = in.adv, diff = lp - (double)in.old, r = (double)exp_of(diff);
     const bool clipped = (A > 0.0 && diff > a.log_high) || (A < 0.0 && diff < a.log_low);      // (a NaN stays in the gradient)
     x.policy = clipped ? -(A > 0.0 ? a.high : a.low) * A : -r * A;
     x.clipped = clipped ? 1.0 : 0.0; x.ratio = r; x.entropy = entropy;
     x.g = clipped ? 0.0 : -r * A;
     if (a.ref) {
         // e^d - 1 and e^d - 1 - d: their series where they would cancel
-        const double d = (double)a.ref[n] - lp;
+        const double d = (double)in.ref - lp;
         double e1, e2;
         if (fabs(d) < 0.5) {
             double p = 1.0 / 39916800;
@@ -216,7 +262,10 @@ __device__ __forceinline__ int policy_target(const PolicyArgs& a, int64_t n)
 // happens in registers; all its lanes carry out the row's 64-bit arithmetic together.
 // ---------------------------------------------------------------------------
 enum { DO_SUMS, DO_GRADIENT, DO_POLICY };
-struct LaneArgs { int lanes; SumArgs s; GradArgs g; PolicyArgs p; };
+template <int DO> struct LaneArgs;
+template <> struct LaneArgs<DO_SUMS> { SumArgs s; int lanes; __device__ const Rows& rows() const { return s.r; } };
+template <> struct LaneArgs<DO_GRADIENT> { GradArgs g; int lanes; __device__ const Rows& rows() const { return g.r; } };
+template <> struct LaneArgs<DO_POLICY> { PolicyArgs p; int lanes; __device__ const Rows& rows() const { return p.r; } };
 
 template <class E, int NE, bool VECTOR>
 struct LaneRow {
@@ -271,29 +320,37 @@ struct LaneRow {
     }
 };
 template <bool FINE, int NE>
-__device__ __forceinline__ Part lanes_part(const float (&z)[NE], const Rows& r, int lanes)
+__device__ __forceinline__ Sums lanes_part(const float (&z)[NE], const Rows& r, int lanes)
 {
     float m = max_of(z, -INFINITY);
     for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     Part p{m, 0.0f, 0.0f};
     add_at<FINE>(p, z, m == -INFINITY ? 0.0f : m, shift_of(m, r.c), r.c, r.c_lo);
+    if (FINE) {
+        double d = fma(LN2, (double)p.u, (double)p.s);
+        for (int off = 1; off < lanes; off <<= 1) d += __shfl_xor(d, off, 64);
+        return Sums{m, d, 0.0};
+    }
     for (int off = 1; off < lanes; off <<= 1) { p.s += __shfl_xor(p.s, off, 64); p.u += __shfl_xor(p.u, off, 64); }
-    return p;
+    return Sums{m, (double)p.s, (double)p.u};
 }
 
 template <class E, int DO, int NE, bool VECTOR, bool FINE>
-__global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs a)
+__global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
 {
     typedef typename E::T T;
     typedef LaneRow<E, NE, VECTOR> L;
-    __shared__ double lds[WG / 64];
-    const Rows& r = DO == DO_SUMS ? a.s.r : DO == DO_GRADIENT ? a.g.r : a.p.r;
+    __shared__ FinishLds lds;
+    const Rows& r = a.rows();
     const int lanes = a.lanes, l = threadIdx.x & (lanes - 1), per = WG / lanes, V = r.V;
-    if (DO == DO_GRADIENT && a.g.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.g.fin, lds); return; }
-    const int64_t grid = DO == DO_GRADIENT && a.g.fin.stats ? gridDim.x - 1 : gridDim.x;
+    int64_t grid = gridDim.x;
+    if constexpr (DO == DO_GRADIENT) {
+        if (a.g.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.g.fin, lds); return; }
+        if (a.g.fin.stats) grid -= 1;
+    }
     double inv = 0.0, v[STATS] = {};
-    if (DO == DO_POLICY) {
-        const double W = block_sum(weight_share(a.p.norm, r, threadIdx.x, WG), lds);
+    if constexpr (DO == DO_POLICY) {
+        const double W = block_sum(weight_share(a.p.norm, r, threadIdx.x, WG), lds.weights);
         inv = W != 0.0 ? a.p.p.grad_scale / W : 0.0;
     }
     for (int64_t base = (int64_t)blockIdx.x * per; base < r.rows; base += grid * per) {
@@ -302,7 +359,7 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs a)
         const T* row = static_cast<const T*>(r.logits) + (there ? n : 0) * r.stride;
         int target = -1;
         float z[NE], d[NE];
-        if (DO == DO_GRADIENT) {
+        if constexpr (DO == DO_GRADIENT) {
             if (!there) continue;
             const RowGrad q = grad_of_row(a.g, n);
             target = q.target;
@@ -312,27 +369,29 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs a)
                 for (int k = 0; k < NE; ++k) d[k] = 0.0f;
             }
             L::store(static_cast<T*>(a.g.out) + n * a.g.out_stride, V, lanes, l, d, target, q.to_target);
-            continue;
-        }
-        if (there) target = DO == DO_SUMS ? row_target(r, n) : policy_target(a.p, n);
+        } else {
+        PolicyIn in{};
+        if constexpr (DO == DO_POLICY) {
+            if (there) target = policy_target(a.p, n);
+            if (target >= 0) in = policy_in(a.p.p, n);
+        } else if (there) target = row_target(r, n);
         if (target >= 0) L::load(row, V, lanes, l, z);
         else {
 #pragma unroll
             for (int k = 0; k < NE; ++k) z[k] = 0.0f;
         }
-        const Part p = lanes_part<FINE>(z, r, lanes);
+        const Sums p = lanes_part<FINE>(z, r, lanes);
         const float chosen = target >= 0 ? E::get(row + target) : 0.0f;
-        if (DO == DO_SUMS) {
+        if constexpr (DO == DO_SUMS) {
             if (there && l == 0) store_sums<FINE>(a.s, n, p, target, chosen);
-            continue;
-        }
+        } else {
         RowGrad q{};
         double lp = 0.0;
         q.target = -1;
         if (target >= 0) {
             const RowSum x = finish_row<false>(p, r);
             lp = logp_of<false>(x, chosen, r);
-            const PolicyRow y = policy_row(a.p.p, n, lp, x.entropy, x.empty);
+            const PolicyRow y = policy_row(a.p.p, in, lp, x.entropy, x.empty);
             if (l == 0) add_stats(v, y);
             q = row_gradient(x, y.g * inv, y.e * inv, target, r.scale);
         }
@@ -344,32 +403,51 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs a)
             for (int k = 0; k < NE; ++k) d[k] = 0.0f;
         }
         L::store(static_cast<T*>(a.p.out) + n * a.p.out_stride, V, lanes, l, d, target, q.to_target);
+        }
+        }
     }
-    if (DO == DO_POLICY) block_partial(v, lds, a.p.parts + blockIdx.x);
+    if constexpr (DO == DO_POLICY) {
+        const int lane = threadIdx.x & 63;
+        block_stats(wave_stats(v), stat_of(lane), (lane & 7) == 0, lds.waves, lds.sums);
+        if (threadIdx.x < STATS) a.p.parts[blockIdx.x].v[threadIdx.x] = lds.sums[threadIdx.x];
+    }
 }
 
 // ---------------------------------------------------------------------------
 // Long rows, a workgroup each.  Sums: one pass with every thread's own running maximum; bound by the read.
 // ---------------------------------------------------------------------------
+// (lane 0 of the first wavefront has the result; the number of wavefronts is a power of two)
 template <bool FINE>
-__device__ __forceinline__ Part block_joined(Part p, float c, float c_lo, Part* lds)
+__device__ __forceinline__ Sums block_joined(Part p, float c, float c_lo, Part* lds, double* lds_s)
 {
-    p = lanes_joined<FINE>(p, c, c_lo, 64);
-    const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const int waves = blockDim.x >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (!FINE) {
+        p = lanes_joined<FINE>(p, c, c_lo, 64);
+        if (lane == 0) lds[wave] = p;
+        __syncthreads();
+        if (lane < waves) p = lds[lane];
+        p = lanes_joined<FINE>(p, c, c_lo, waves);
+        return Sums{p.m, (double)p.s, (double)p.u};
+    }
+    float m = p.m;
+    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    if (lane == 0) lds[wave].m = m;
     __syncthreads();
-    if (lane == 0) lds[threadIdx.x >> 6] = p;
-    __syncthreads();
-    if (lane < waves) p = lds[lane];
-    return lanes_joined<FINE>(p, c, c_lo, waves);                       // (lane 0 has it; waves is a power of two)
+    for (int w = 0; w < waves; ++w) m = fmaxf(m, lds[w].m);
+    rescale<FINE>(p, m, c, c_lo);
+    return Sums{m, block_sum(fma(LN2, (double)p.u, (double)p.s), lds_s), 0.0};
 }
 template <class E, bool FINE>
 __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
 {
     __shared__ Part lds[16];
+    __shared__ double lds_s[16];
     const int64_t n = blockIdx.x;
     const int target = row_target(a.r, n), V = a.r.V, nt = blockDim.x;
     const typename E::T* row = static_cast<const typename E::T*>(a.r.logits) + n * a.r.stride;
+    const float chosen = target >= 0 ? E::get(row + target) : 0.0f;
     Part p{-INFINITY, 0.0f, 0.0f};
+    Sums sums{};
     if (target >= 0) {
         constexpr int U = 4;                                            // loads in flight
         const int vecs = V / E::N;
@@ -398,9 +476,9 @@ __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
             const float z[1] = {E::get(row + j)};
             add_elements<FINE>(p, z, c, c_lo);
         }
-        p = block_joined<FINE>(p, c, c_lo, lds);
+        sums = block_joined<FINE>(p, c, c_lo, lds, lds_s);
     }
-    if (threadIdx.x == 0) store_sums<FINE>(a, n, p, target, target >= 0 ? E::get(row + target) : 0.0f);
+    if (threadIdx.x == 0) store_sums<FINE>(a, n, sums, target, chosen);
 }
 
 // ---------------------------------------------------------------------------
@@ -411,7 +489,7 @@ template <class E, bool ENT>
 __global__ __launch_bounds__(WG) void block_gradients(const GradArgs a)
 {
     typedef typename E::T T;
-    __shared__ double lds[WG / 64];
+    __shared__ FinishLds lds;
     if (a.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.fin, lds); return; }
     const int64_t n = a.r.rows - 1 - blockIdx.x;
     const RowGrad q = grad_of_row(a, n);
@@ -481,6 +559,10 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
         }
         return;
     }
+    // (loads return in order: the few small ones first)
+    PolicyIn in{};
+    if (tid == 0) in = policy_in(a.p, n);
+    double share = weight_share(a.norm, a.r, tid, NT);
     u32x4_any w[VPT];
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
@@ -488,7 +570,7 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
     const int j_tail = vecs * E::N + tid;
     const float z_tail = j_tail < V ? E::get(row + j_tail) : -INFINITY;
     const float chosen = E::get(row + target);
-    const double share = wave_sum(weight_share(a.norm, a.r, tid, NT));
+    share = wave_sum(share);
     // maximum of the wavefront's pieces, then their sums at that shift
     const float c = a.r.c, c_lo = a.r.c_lo;
     float m = z_tail;
@@ -515,9 +597,9 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
         p = lanes_joined<false>(p, c, c_lo, WAVES);
         const double W = wave_sum(lane < WAVES ? weights[lane] : 0.0);
         if (lane == 0) {
-            const RowSum x = finish_row<false>(p, a.r);
+            const RowSum x = finish_row<false>(Sums{p.m, (double)p.s, (double)p.u}, a.r);
             const double lp = logp_of<false>(x, chosen, a.r), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
-            const PolicyRow y = policy_row(a.p, n, lp, x.entropy, x.empty);
+            const PolicyRow y = policy_row(a.p, in, lp, x.entropy, x.empty);
             row_grad = row_gradient(x, y.g * inv, y.e * inv, target, a.r.scale);
             if (a.logp) a.logp[n] = (float)lp;
             double v[STATS] = {};
@@ -568,43 +650,54 @@ struct PairArgs {
 };
 __global__ __launch_bounds__(WG) void pair_sums(const PairArgs a)
 {
-    __shared__ double lds[WG / 64];
+    __shared__ FinishLds lds;
     const int64_t P = a.q.count / 2;
-    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, WG), lds), inv = W != 0.0 ? a.grad_scale / W : 0.0;
+    const int lane = threadIdx.x & 63;
+    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, WG), lds.weights), inv = W != 0.0 ? a.grad_scale * reciprocal(W) : 0.0;
     double v[STATS] = {};
     for (int64_t k = blockIdx.x; k < P; k += gridDim.x) {
         const Seq s[2] = {sequence(a.q, k), sequence(a.q, k + P)};
-        double D[2], n[2];
+        double t[STATS] = {};                                           // of the first and of the second: sum, tokens
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            double d = 0.0, c = 0.0;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll 2
             for (int64_t j = threadIdx.x; j < s[i].n; j += WG) {
                 const int64_t row = s[i].first + j * s[i].step;
-                if (a.ws[row].target >= 0) { d += a.ws[row].lp - (a.ref ? (double)a.ref[row] : 0.0); c += 1.0; }
+                const RowWs w = a.ws[row];
+                const float ref = a.ref ? a.ref[row] : 0.0f;
+                if (w.target >= 0) { t[2 * i] += w.lp - (double)ref; t[2 * i + 1] += 1.0; }
             }
-            D[i] = block_sum(d, lds); n[i] = block_sum(c, lds);
-            if (a.mean) D[i] = n[i] > 0.0 ? D[i] / n[i] : 0.0;
-            if (s[i].broken) D[i] = NAN;
+        block_stats(wave_stats(t), stat_of(lane), (lane & 7) == 0, lds.waves, lds.sums);
+        double D[2], per[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            per[i] = a.mean && lds.sums[2 * i + 1] > 0.0 ? reciprocal(lds.sums[2 * i + 1]) : 1.0;
+            D[i] = s[i].broken ? (double)NAN : lds.sums[2 * i] * per[i];
         }
+        const double n = lds.sums[1] + lds.sums[3];
         const double h = a.beta * (D[0] - D[1]) - a.margin, y = a.label ? (double)a.label[k] : 1.0, w = a.weight ? (double)a.weight[k] : 1.0;
         if (a.margins && threadIdx.x == 0) a.margins[k] = (float)h;
+        __syncthreads();                                                // (sums are read before the next pair's are written)
         if (w == 0.0) continue;
-        const double e = exp(-fabs(h)), up = 1.0 / (1.0 + e), down = e / (1.0 + e);                 // sigmoid(|h|), sigmoid(-|h|)
-        const double soft = log1p(e), sig = h >= 0.0 ? up : down, gis = h >= 0.0 ? down : up;
-        const double lossy = y != 0.0 ? y * (soft + fmax(-h, 0.0)) : 0.0, lossn = y != 1.0 ? (1.0 - y) * (soft + fmax(h, 0.0)) : 0.0;
+        const double e = (double)exp_of(-fabs(h)), up = reciprocal(1.0 + e), down = e * up;         // sigmoid(|h|), sigmoid(-|h|)
+        const double soft = e < 1e-4 ? e * (1.0 - 0.5 * e) : log_of_sum(1.0 + e);                   // ln(1 + e^-|h|)
+        const double sig = h >= 0.0 ? up : down, gis = h >= 0.0 ? down : up;
         const double dh = w * a.beta * ((1.0 - y) * sig - y * gis) * inv;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float g = (float)((i == 0 ? dh : -dh) / (a.mean ? (n[i] > 0.0 ? n[i] : 1.0) : 1.0));
+            const float g = (float)((i == 0 ? dh : -dh) * per[i]);
             for (int64_t j = threadIdx.x; j < s[i].n; j += WG) a.to_logp[s[i].first + j * s[i].step] = g;
         }
         if (threadIdx.x == 0) {
             const double nan = h != h ? (double)NAN : 0.0;
+            const double lossy = y != 0.0 ? y * (soft + fmax(-h, 0.0)) : 0.0, lossn = y != 1.0 ? (1.0 - y) * (soft + fmax(h, 0.0)) : 0.0;
             v[0] += w * (lossy + lossn) + nan; v[1] += w * (h > 0.0 ? 1.0 : 0.0); v[2] += w * a.beta * D[0]; v[3] += w * a.beta * D[1]; v[4] += w * h;
-            v[6] += 1.0; v[7] += n[0] + n[1];
+            v[6] += 1.0; v[7] += n;
         }
     }
-    block_partial(v, lds, a.parts + blockIdx.x);
+    if (threadIdx.x == 0)                                               // (the pairs' sums are that thread's alone)
+#pragma unroll
+        for (int k = 0; k < STATS; ++k) a.parts[blockIdx.x].v[k] = v[k];
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -625,7 +718,7 @@ static LaneForm lane_form(int type, int64_t V);
 constexpr int MAX_PARTS = 2048;                   // workgroups of short rows (8 for every compute unit) and of pairs that report sums at most
 
 // log-probabilities need none; the clipped loss room for the weights' and the workgroups' sums; pairs rows of their own too
-struct RowsWs { size_t weights, parts, ws, to_logp, total; };
+struct RowsWs { size_t weights, parts, folded, ws, to_logp, total; };
 static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
 {
     RowsWs w;
@@ -634,6 +727,7 @@ static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
     w.weights = take(WEIGHT_PARTS * sizeof(double));
     const bool lanes = lane_form(ANAKIN_TYPE_FP32, vocab).lanes > 0;    // (fp32 rows are the first to take workgroups)
     w.parts = take((size_t)(!lanes && rows > MAX_PARTS ? rows : MAX_PARTS) * sizeof(Partial));
+    w.folded = take(FOLDED * sizeof(Partial));
     w.ws = take(pairs ? (size_t)rows * sizeof(RowWs) : 0);
     w.to_logp = take(pairs ? (size_t)rows * 4 : 0);
     w.total = off;
@@ -703,7 +797,7 @@ static unsigned lane_grid(const LaneForm& f, int64_t rows)
     return (unsigned)(g < 1 ? 1 : g > MAX_PARTS ? MAX_PARTS : g);
 }
 template <class E, int DO, bool FINE>
-static void launch_lanes(const LaneForm& f, const LaneArgs& a, unsigned grid, hipStream_t s)
+static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid, hipStream_t s)
 {
     auto k = f.pieces == 0 ? lanes_rows<E, DO, 4, false, FINE> : f.pieces == 1 ? lanes_rows<E, DO, E::N, true, FINE> : lanes_rows<E, DO, 4 * E::N, true, FINE>;
     hipLaunchKernelGGL(k, dim3(grid), dim3(WG), 0, s, a);
@@ -715,15 +809,15 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
     if (a.r.rows == 0) return hipSuccess;
     const LaneForm f = lane_form(type, a.r.V);
     if (f.lanes) {
-        LaneArgs l{};
+        LaneArgs<DO_SUMS> l{};
         l.lanes = f.lanes; l.s = a;
         if (fine) BY_TYPE(type, launch_lanes, DO_SUMS, true)(f, l, lane_grid(f, a.r.rows), s);
         else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
     } else {
-        // few rows: as many threads to a row as there are
-        const dim3 block(a.r.rows <= 512 ? 1024 : 256);
-        if (fine) hipLaunchKernelGGL(BY_TYPE(type, block_sums, true), dim3((unsigned)a.r.rows), block, 0, s, a);
-        else hipLaunchKernelGGL(BY_TYPE(type, block_sums, false), dim3((unsigned)a.r.rows), block, 0, s, a);
+        // Few rows: as many threads to a row as there are (one row of 131072 bf16 24 -> 13 us).  A compute unit's arithmetic
+        // bounds such a row, 8 us; sharing it out would take a second launch, which costs the host 3 us.
+        const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 512 ? 1024 : 256);
+        hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
     }
     return hipGetLastError();
 }
@@ -733,7 +827,7 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
     const LaneForm f = lane_form(type, a.r.V);
     if (a.r.rows == 0 && !more) return hipSuccess;
     if (f.lanes) {
-        LaneArgs l{};
+        LaneArgs<DO_GRADIENT> l{};
         l.lanes = f.lanes; l.g = a;
         BY_TYPE(type, launch_lanes, DO_GRADIENT, false)(f, l, lane_grid(f, a.r.rows) + more, s);
     } else if (ent) hipLaunchKernelGGL(BY_TYPE(type, block_gradients, true), dim3((unsigned)a.r.rows + more), dim3(WG), 0, s, a);
@@ -758,7 +852,7 @@ static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipSt
     if (a.r.rows == 0) return hipSuccess;
     const LaneForm f = lane_form(type, a.r.V);
     if (f.lanes) {
-        LaneArgs l{};
+        LaneArgs<DO_POLICY> l{};
         l.lanes = f.lanes; l.p = a;
         const unsigned grid = lane_grid(f, a.r.rows);
         *parts = (int)grid;
@@ -777,7 +871,7 @@ static hipError_t launch_weights(const Rows& r, int64_t n, const float* weight, 
     if (norm != 0.0 || n == 0) return hipSuccess;
     if (pairs && !weight) { w.norm = (double)n; return hipSuccess; }
     if (!pairs && n <= INLINE_ROWS) { w.inline_rows = (int)n; return hipSuccess; }
-    const int64_t g = (n + 4 * WG - 1) / (4 * WG);
+    const int64_t g = (n + WG - 1) / WG;
     w.n_parts = (int)(g > WEIGHT_PARTS ? WEIGHT_PARTS : g);
     hipLaunchKernelGGL(weight_sums, dim3(w.n_parts), dim3(WG), 0, s, r, n, weight, pairs, parts);
     return hipGetLastError();
@@ -796,13 +890,11 @@ extern "C" size_t anakin_rows_workspace_bytes(int64_t rows, int64_t vocab, int64
     return rows_workspace(rows, vocab, pairs).total;
 }
 
-extern "C" int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy,
-                                         void* d_workspace, size_t workspace_bytes, void* hip_stream)
+extern "C" int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy, void* hip_stream)
 {
     SumArgs a{};
     TRY(check_rows(x, a.r));
     if (x->rows > 0 && (!d_logp || !d_lse)) return fail(ANAKIN_E_INVALID_ARG, "null logp or lse");
-    TRY(check_workspace(d_workspace, workspace_bytes, rows_workspace(x->rows, x->vocab, 0).total));
     a.logp = d_logp; a.lse = d_lse; a.entropy = d_entropy;
     LAUNCH(launch_sums(x->type, a, false, static_cast<hipStream_t>(hip_stream)));
     return ANAKIN_OK;
@@ -848,8 +940,14 @@ extern "C" int32_t anakin_policy_loss(const anakin_rows* x, const anakin_policy_
     LAUNCH(launch_weights(r, x->rows, a->d_weight, false, a->norm, reinterpret_cast<double*>(base + w.weights), p.norm, s));
     int parts = 0;
     LAUNCH(launch_policy(x->type, p, &parts, s));
-    const FinishArgs f{p.parts, parts, r, p.norm, a->d_stats, a->kl_coef, a->entropy_coef, 1};
-    hipLaunchKernelGGL(finish_stats, dim3(1), dim3(parts > 64 ? FINISH_WG : 64), 0, s, f);
+    FinishArgs f{p.parts, parts, r, p.norm, a->d_stats, a->kl_coef, a->entropy_coef, 1};
+    if (parts > FOLD_FROM) {
+        Partial* folded = reinterpret_cast<Partial*>(base + w.folded);
+        hipLaunchKernelGGL(fold_stats, dim3(FOLDED), dim3(WG), 0, s, p.parts, parts, folded);
+        LAUNCH(hipGetLastError());
+        f.parts = folded; f.n_parts = FOLDED;
+    }
+    hipLaunchKernelGGL(finish_stats, dim3(1), dim3(FINISH_WG), 0, s, f);
     LAUNCH(hipGetLastError());
     return ANAKIN_OK;
 }
@@ -905,7 +1003,7 @@ extern "C" int32_t anakin_preference_loss(const anakin_rows* x, const anakin_seq
         g.r = r; g.out = a->d_dlogits; g.out_stride = a->grad_stride; g.ws = p.ws; g.to_logp = p.to_logp; g.fin = f;
         LAUNCH(launch_gradients(x->type, g, false, s));
     } else {
-        hipLaunchKernelGGL(finish_stats, dim3(1), dim3(blocks > 64 ? FINISH_WG : 64), 0, s, f);
+        hipLaunchKernelGGL(finish_stats, dim3(1), dim3(FINISH_WG), 0, s, f);
         LAUNCH(hipGetLastError());
     }
     return ANAKIN_OK;

@@ -101,7 +101,7 @@ class _Call:
             return None
         if t.device != self.device:
             _refuse(f"{name} is on another device")
-        if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
             _refuse(f"{name} has to be contiguous {dtype} [{n}]")
         return t.data_ptr()
 
@@ -134,11 +134,13 @@ class _Call:
         return torch.empty(n, dtype=dtype, device=self.device)
 
     def run(self, function, *args):
-        if torch.cuda.current_device() == self.device.index:
-            rc = function(*args, torch.cuda.current_stream(self.device).cuda_stream)
+        index = self.device.index
+        stream = torch._C._cuda_getCurrentRawStream(index)             # the current stream's handle, without an object around it
+        if torch.cuda.current_device() == index:
+            rc = function(*args, stream)
         else:
-            with torch.cuda.device(self.device):
-                rc = function(*args, torch.cuda.current_stream(self.device).cuda_stream)
+            with torch.cuda.device(index):
+                rc = function(*args, stream)
         if rc != binding.OK:
             raise AnakinError(rc, self.L.anakin_last_error(None).decode())
 
@@ -150,8 +152,7 @@ def logprobs(logits, target, scale=1.0, entropy=False):
     x = c.rows(logits, target, scale)
     logp, lse = c.empty(x.rows), c.empty(x.rows)
     h = c.empty(x.rows) if entropy else None
-    ws = c.empty(c.L.anakin_rows_workspace_bytes(x.rows, x.vocab, 0), torch.uint8)
-    c.run(c.L.anakin_token_logprobs, x, logp.data_ptr(), lse.data_ptr(), h.data_ptr() if entropy else None, ws.data_ptr(), ws.numel())
+    c.run(c.L.anakin_token_logprobs, x, logp.data_ptr(), lse.data_ptr(), h.data_ptr() if entropy else None)
     return LogProbs(logp, lse, h)
 
 

@@ -235,7 +235,7 @@ def test_rows_are_checked_on_the_host(lib, over):
     x = _rows(**over)
     assert lib.anakin_policy_loss(x, _policy(), FAKE, 1 << 30, None) == binding.E_INVALID_ARG
     assert lib.anakin_last_error(None)
-    assert lib.anakin_token_logprobs(x, FAKE, FAKE, None, FAKE, 1 << 30, None) == binding.E_INVALID_ARG
+    assert lib.anakin_token_logprobs(x, FAKE, FAKE, None, None) == binding.E_INVALID_ARG
     assert lib.anakin_token_logprobs_backward(x, FAKE, None, FAKE, None, FAKE + 0x200000, 100, None) == binding.E_INVALID_ARG
 
 
@@ -259,9 +259,9 @@ def test_workspaces_are_checked_on_the_host(lib):
     for bad in ((-1, 5, 0), (5, 0, 0), (1 << 31, 5, 0), (5, 1 << 28, 0), (5, 5, -1)):
         assert lib.anakin_rows_workspace_bytes(*bad) == 0
     assert lib.anakin_returns_workspace_bytes(-1, 1) == 0 and lib.anakin_returns_workspace_bytes(1, -1) == 0
-    assert lib.anakin_token_logprobs(_rows(logits=FAKE + 1), FAKE, FAKE, None, FAKE, 1 << 30, None) == binding.E_MISALIGNED
-    assert lib.anakin_token_logprobs(_rows(target=FAKE + 4), FAKE, FAKE, None, FAKE, 1 << 30, None) == binding.E_MISALIGNED
-    assert lib.anakin_token_logprobs(_rows(), None, FAKE, None, FAKE, 1 << 30, None) == binding.E_INVALID_ARG
+    assert lib.anakin_token_logprobs(_rows(logits=FAKE + 1), FAKE, FAKE, None, None) == binding.E_MISALIGNED
+    assert lib.anakin_token_logprobs(_rows(target=FAKE + 4), FAKE, FAKE, None, None) == binding.E_MISALIGNED
+    assert lib.anakin_token_logprobs(_rows(), None, FAKE, None, None) == binding.E_INVALID_ARG
     assert lib.anakin_token_logprobs_backward(_rows(), FAKE, None, FAKE, FAKE, FAKE + 0x200000, 100, None) == binding.E_INVALID_ARG
     assert lib.anakin_token_logprobs_backward(_rows(), FAKE, None, FAKE, None, None, 100, None) == binding.E_INVALID_ARG
 
