@@ -246,9 +246,30 @@ int32_t anakin_set_update_chunk_mode(anakin_t* h, int32_t mode);
  * value and entropy terms stay as they are, the reported policy loss becomes minus the mean
  * reward.  Pendulum with the tanh-Gaussian policy, fp32 net of two equal hidden layers of 64, 128
  * or 256 units, B a multiple of 16, one update per unroll: ANAKIN_E_BAD_CONFIG otherwise (for the
- * last, from anakin_learn).  Kept until changed. */
-enum { ANAKIN_PG_SCORE_FUNCTION = 0, ANAKIN_PG_PATHWISE = 1 };
+ * last, from anakin_learn).  Kept until changed.
+ * ANAKIN_PG_CLIPPED: the clipped policy loss of anakin_policy_loss in place of policy and entropy term, with the policy
+ * that acted as old policy and as reference of the KL term (coefficients: anakin_set_clip; entropy_coef as ever).  It is
+ * what several updates per unroll want in the sequential mode, where the policy moves away from the one that acted; at
+ * the acting parameters its ratio is 1 and its gradient the score function's.  The reported policy loss is the clipped
+ * term plus kl_coef times the KL term.
+ * ANAKIN_PG_PREFERENCE: the loss of anakin_preference_loss in place of policy and entropy term: environments b and
+ * b + B / 2 are a pair, a chunk's steps (all T with one update per unroll) their sequences, the policy that acted is the
+ * reference (beta, labels: anakin_set_preference).  The reported policy loss is that loss.
+ * Both: categorical policies (Catch, maze); ANAKIN_E_BAD_CONFIG otherwise, and from decoupled steps.  Returns,
+ * advantages and the value's term stay as they are. */
+enum { ANAKIN_PG_SCORE_FUNCTION = 0, ANAKIN_PG_PATHWISE = 1, ANAKIN_PG_CLIPPED = 2, ANAKIN_PG_PREFERENCE = 3 };
 int32_t anakin_set_policy_gradient(anakin_t* h, int32_t kind);
+
+/* Coefficients of ANAKIN_PG_CLIPPED: 0 <= clip_low <= 1, 0 <= clip_high, default 0.2 both; kl_coef, default 0.
+ * ANAKIN_E_INVALID_ARG otherwise.  Kept until changed. */
+int32_t anakin_set_clip(anakin_t* h, double clip_low, double clip_high, double kl_coef);
+
+/* Coefficients of ANAKIN_PG_PREFERENCE.  beta (default 0.1).  d_label, d_weight: fp32 [chunks][B / 2] in device memory, read
+ * by every anakin_learn from then on (row k by update k of an unroll; ANAKIN_E_STATE from anakin_learn if it has more
+ * updates than that): how far environment b of pair b is preferred over b + B / 2, in [0, 1],
+ * and the pair's weight (0: left out).  d_weight null: 1.  d_label null: 1 where the sum of rewards of environment b over
+ * the chunk is the larger one, 0 where it is the smaller one, 1/2 where they are equal. */
+int32_t anakin_set_preference(anakin_t* h, double beta, const float* d_label, const float* d_weight, int32_t chunks);
 
 /* How the update of this handle is cut into workgroups (what the parity tests assert their cases reach, and
  * what the benchmark prints).  splits[l], l < n_hidden: chunks of the B*T samples whose partial dW_{l+1} / db_{l+1}
@@ -328,7 +349,7 @@ typedef struct {
     double scale;
 } anakin_rows;
 
-/* logp[n] = log softmax(scale * logits[n])[target[n]], lse[n] = log sum exp(scale * logits[n]), and (where not null)
+/* logp[n] = log softmax(scale * logits[n])[target[n]], and (where not null) lse[n] = log sum exp(scale * logits[n]),
  * entropy[n] = -sum p log p.  Rows that take no part get zeros; a row all of whose logits are minus infinity gets
  * logp = lse = -inf and entropy 0. */
 int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy, void* hip_stream);

@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("ANAKIN_LIB", os.path.join(_HERE, "libanakin.so"))
 OK = 0
 E_INVALID_ARG, E_BAD_CONFIG, E_WORKSPACE_TOO_SMALL, E_MISALIGNED, E_HIP, E_NONFINITE, E_STATE = -1, -2, -3, -4, -5, -6, -7
 MODE_VALU_GEMM, MODE_CANONICAL_ACTING, MODE_STREAM_WEIGHTS = 1, 2, 4
-PG_SCORE_FUNCTION, PG_PATHWISE = 0, 1
+PG_SCORE_FUNCTION, PG_PATHWISE, PG_CLIPPED, PG_PREFERENCE = 0, 1, 2, 3
 CHUNKS_AT_ACTING_PARAMETERS, CHUNKS_SEQUENTIAL = 0, 1
 STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -93,7 +93,7 @@ EXPORTS = ["anakin_workspace_bytes", "anakin_create", "anakin_rollout", "anakin_
            "anakin_destroy", "anakin_param_count", "anakin_get_params", "anakin_set_params", "anakin_get_grads",
            "anakin_get_opt_state", "anakin_set_opt_state", "anakin_get_env_state", "anakin_set_env_state",
            "anakin_get_walls", "anakin_get_global_step", "anakin_set_global_step", "anakin_get_trajectory",
-           "anakin_get_metrics", "anakin_get_plan", "anakin_set_mode", "anakin_set_updates_per_unroll", "anakin_set_update_chunk_mode", "anakin_set_policy_gradient", "anakin_profile", "anakin_kernel_times", "anakin_peak_probe",
+           "anakin_get_metrics", "anakin_get_plan", "anakin_set_mode", "anakin_set_updates_per_unroll", "anakin_set_update_chunk_mode", "anakin_set_policy_gradient", "anakin_set_clip", "anakin_set_preference", "anakin_profile", "anakin_kernel_times", "anakin_peak_probe",
            "anakin_rows_workspace_bytes", "anakin_token_logprobs", "anakin_token_logprobs_backward", "anakin_policy_loss", "anakin_preference_loss",
            "anakin_returns_workspace_bytes", "anakin_lambda_returns",
            "anakin_last_error"]
@@ -141,6 +141,8 @@ def load():
     L.anakin_set_updates_per_unroll.argtypes = [vp, C.c_int32]
     L.anakin_set_update_chunk_mode.argtypes = [vp, C.c_int32]
     L.anakin_set_policy_gradient.argtypes = [vp, C.c_int32]
+    L.anakin_set_clip.argtypes = [vp, C.c_double, C.c_double, C.c_double]
+    L.anakin_set_preference.argtypes = [vp, C.c_double, vp, vp, C.c_int32]
     L.anakin_profile.argtypes = [vp, C.c_int32]
     L.anakin_kernel_times.argtypes = [vp, C.POINTER(KernelTime), C.c_int32, C.POINTER(C.c_int32)]
     L.anakin_last_error.argtypes = [vp]
@@ -246,6 +248,21 @@ class Anakin:
 
     def set_policy_gradient(self, kind):
         self._chk(self.L.anakin_set_policy_gradient(self.h, int(kind)))
+
+    def set_clip(self, clip_low=0.2, clip_high=0.2, kl_coef=0.0):
+        """Coefficients of the clipped policy loss (PG_CLIPPED)."""
+        self._chk(self.L.anakin_set_clip(self.h, clip_low, clip_high, kl_coef))
+
+    def set_preference(self, beta=0.1, label=None, weight=None):
+        """Coefficients of the loss over pairs of environments (PG_PREFERENCE); label, weight: fp32 tensors
+        [updates per unroll][B / 2] on the device (kept alive by this object), None: by the rewards, 1."""
+        given = [t for t in (label, weight) if t is not None]
+        for t in given:
+            if t.device != self.ws.device or str(t.dtype) != "torch.float32" or not t.is_contiguous() or t.dim() != 2 or t.shape[1] != self.B // 2:
+                raise AnakinError(E_INVALID_ARG, "labels and weights have to be contiguous fp32 [updates][B / 2] on the handle's device")
+        self._chk(self.L.anakin_set_preference(self.h, beta, label.data_ptr() if label is not None else None, weight.data_ptr() if weight is not None else None,
+                                               min((t.shape[0] for t in given), default=0)))
+        self._preference = (label, weight)
 
     def set_actor_stream(self, stream):
         """stream: a torch.cuda.Stream the actor of step_decoupled runs on (kept alive by this object)"""

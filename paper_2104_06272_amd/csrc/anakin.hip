@@ -179,6 +179,12 @@ static void carve(const EnvDims& ed, const NetShape& ns, int B, int T, const int
     L.alt_tr_val = take(dec ? t1n * 4 : 0); L.alt_tr_head = take(dec ? t1n * ns.NHP * 4 : 0);
     L.head_new = take(dec ? t1n * ns.NHP * 4 : 0); L.val_new = take(dec ? t1n * 4 : 0); L.eps_new = take(dec ? tn * 4 : 0);
     L.head_old = 0;
+    // token losses: workspace of an operator over the unroll's samples (large ones lie in dz[0], which the backward pass writes
+    // after the loss), statistics of every chunk, labels of the pairs of environments
+    const bool cat = ns.policy == POLICY_CATEGORICAL;
+    const size_t tok = cat ? anakin_rows_workspace_bytes((int64_t)tn, ns.A, 1) : 0;
+    L.tok_ws = tok <= tn * ns.dims[1] * 4 ? 0 : take(tok);
+    L.tok_stats = take(cat ? (size_t)T * 8 * 4 : 0); L.tok_label = take(cat ? n / 2 * 4 : 0);
     L.path = take(ed.kind == ENV_PENDULUM && !ns.bf16 ? tn * 2 * 4 : 0);
     L.small_part = take(small_fused_part_bytes(ed, ns, B, T));
     L.counters = take(256);
@@ -477,6 +483,8 @@ extern "C" int32_t anakin_create(anakin_t** out, const anakin_env_cfg* env, cons
     h->env_cfg = *env; h->net_cfg = *net; h->env = ed; h->net = ns; h->B = B; h->T = T;
     h->seed = seed; h->gstep = 0; h->adam_t = 0; h->have_traj = 0; h->mode = 0; h->prof_on = 0; h->traj_packed = 0; h->traj_no_acts = 0;
     h->pathwise = 0; h->metric_blocks = 0;
+    h->token_loss = 0; h->clip_low = h->clip_high = 0.2; h->kl_coef = 0.0; h->beta = 0.1; h->pair_label = h->pair_weight = nullptr; h->pair_chunks = 0;
+    h->metric_token = 0; h->metric_chunks = 0;
     h->traj_decoupled = 0; h->actor_stream = nullptr; h->actor_stream_owned = 0; h->ev_fork = nullptr; h->ev_join = nullptr;
     h->ws = static_cast<char*>(d_workspace); h->ws_bytes = workspace_bytes;
     h->scratch = nullptr;
@@ -659,10 +667,50 @@ extern "C" int32_t anakin_rollout(anakin_t* h)
     return ANAKIN_OK;
 }
 
+// ---- policy terms by the operators of token policies (a sample of the unroll is a row, its head outputs the logits) --------
+static anakin_rows samples_as_rows(anakin* h, size_t head)
+{
+    return anakin_rows{at<void>(h, head), (int64_t)h->B * h->T, h->net.A, h->net.NHP, at<void>(h, h->lay.tr_act), ANAKIN_TYPE_FP32, ANAKIN_INDEX_U8, 1.0};
+}
+static int32_t token_error(anakin* h, int32_t rc) { if (rc != ANAKIN_OK) h->err = call_error(); return rc; }
+
+// log-probabilities of the stored actions under the policy that took them, for all of the unroll
+static int32_t acting_logprobs(anakin* h)
+{
+    const anakin_rows x = samples_as_rows(h, h->lay.tr_head);
+    ProfScope prof(h, "token_logprobs");
+    return token_error(h, anakin_token_logprobs(&x, at<float>(h, h->lay.eps_new), nullptr, nullptr, h->stream));
+}
+// the policy's part of the head gradient on the samples the layout and T currently describe (chunk k), beside the value's
+static int32_t token_loss(anakin* h, int k)
+{
+    const Layout& L = h->lay;
+    const anakin_rows x = samples_as_rows(h, L.tr_head);
+    const size_t off = L.tok_ws ? L.tok_ws : L.dz[0], need = anakin_rows_workspace_bytes(x.rows, x.vocab, 1);
+    float* logp = at<float>(h, L.eps_new), * stats = at<float>(h, L.tok_stats) + (size_t)k * 8, * dhead = at<float>(h, L.dhead);
+    if (h->token_loss == ANAKIN_PG_CLIPPED) {
+        const anakin_policy_args a{logp, at<float>(h, L.adv), logp, nullptr, h->clip_low, h->clip_high, h->kl_coef, (double)h->net_cfg.entropy_coef,
+                                   (double)x.rows, 1.0, stats, nullptr, dhead, h->net.NHP};
+        ProfScope prof(h, "policy_loss");
+        return token_error(h, anakin_policy_loss(&x, &a, at<void>(h, off), need, h->stream));
+    }
+    const float* label = h->pair_label ? h->pair_label + (size_t)k * (h->B / 2) : at<float>(h, L.tok_label);
+    if (!h->pair_label) HIPCHK(h, launch_segment_labels(h, at<float>(h, L.tok_label)));
+    const anakin_sequences q{ANAKIN_LAYOUT_TIME, h->B, h->T, nullptr, nullptr};
+    const anakin_preference_args a{logp, label, h->pair_weight ? h->pair_weight + (size_t)k * (h->B / 2) : nullptr, h->beta, 0.0, 0.0, 1.0, 0,
+                                   stats, nullptr, nullptr, dhead, h->net.NHP};
+    ProfScope prof(h, "preference_loss");
+    return token_error(h, anakin_preference_loss(&x, &q, &a, at<void>(h, off), need, h->stream));
+}
+
 // loss, backward pass and Adam on the samples the handle's layout and T currently describe
-static int32_t run_update(anakin* h, bool loss_done = false)
+static int32_t run_update(anakin* h, bool loss_done = false, int chunk = 0)
 {
     if (!loss_done) HIPCHK(h, launch_head_grad(h));
+    if (h->token_loss) {
+        const int32_t rc = token_loss(h, chunk);
+        if (rc != ANAKIN_OK) return rc;
+    }
     if (h->traj_packed) HIPCHK(h, launch_backward_bf16(h));
     else if (one_layer_learn(h)) HIPCHK(h, launch_learn_one_layer(h));
     else HIPCHK(h, launch_backward(h));
@@ -677,6 +725,11 @@ extern "C" int32_t anakin_learn(anakin_t* h)
     if (h->traj_decoupled) { h->err = "the stored unroll was collected by a decoupled step (older parameters, no activations): continue with anakin_step_decoupled"; return ANAKIN_E_STATE; }
     if (h->traj_packed != (bf16_mfma(h) ? 1 : 0)) { h->err = "the mode changed between rollout and learn"; return ANAKIN_E_STATE; }
     if (h->traj_no_acts != (one_layer_fused(h) ? 1 : 0)) { h->err = "the mode changed between rollout and learn"; return ANAKIN_E_STATE; }
+    if (h->token_loss == ANAKIN_PG_PREFERENCE && (h->pair_label || h->pair_weight) && h->n_updates > h->pair_chunks) {
+        h->err = "the preferences have fewer rows than the unroll has updates";
+        return ANAKIN_E_STATE;
+    }
+    h->metric_token = 0;
     if (catch_fused_ok(h)) {
         // scan, loss, backward pass in one launch; then Adam over as many partial sums as that has workgroups
         const int chunks[2] = {h->splits[0], h->splits[1]};
@@ -701,6 +754,11 @@ extern "C" int32_t anakin_learn(anakin_t* h)
         if (h->n_updates != 1) { h->err = "the pathwise policy gradient takes one update per unroll (chunks would cut the adjoint)"; return ANAKIN_E_BAD_CONFIG; }
         HIPCHK(h, launch_pathwise(h));
     }
+    if (h->token_loss) {
+        const int32_t rc = acting_logprobs(h);
+        if (rc != ANAKIN_OK) return rc;
+    }
+    h->metric_token = h->token_loss; h->metric_chunks = h->n_updates;
     if (h->n_updates == 1) {
         int32_t rc = run_update(h, fused_loss);
         if (rc != ANAKIN_OK) return rc;
@@ -741,6 +799,7 @@ extern "C" int32_t anakin_learn(anakin_t* h)
         L.tr_act += r0; L.tr_eps += r0 * 4; L.tr_actf += r0 * 4; L.tr_rew += r0 * 4; L.tr_done += r0;
         L.tr_val += r0 * 4; L.tr_head += r0 * n.NHP * 4;
         L.adv += r0 * 4; L.ret += r0 * 4;
+        if (h->token_loss) L.eps_new += r0 * 4;                       // the actions' log-probabilities at acting time
         for (int l = 0; l < n.L; ++l) { L.act[l] += r0 * n.dims[l + 1] * (h->traj_packed ? 2 : 4); L.mask[l] += r0 * n.dims[l + 1] / 4; }
         L.loss_part += (size_t)k * h->sub_loss_blocks * 8 * 4;
         if (seq && k > 0) {
@@ -751,7 +810,7 @@ extern "C" int32_t anakin_learn(anakin_t* h)
             if (e != hipSuccess) { h->err = std::string("replay of the forward pass: ") + hipGetErrorString(e); rc = ANAKIN_E_HIP; break; }
             L.head_old = L.tr_head; L.tr_head = L.head_new;
         }
-        rc = run_update(h);
+        rc = run_update(h, false, k);
         for (int l = 0; l < MAX_REGIONS; ++l) { h->splits[l] = full_splits[l]; h->quanta[l] = full_quanta[l]; }
         h->splits_w = full_sw; h->head_fan = full_fan; h->loss_blocks = full_lb;
     }
@@ -792,12 +851,38 @@ extern "C" int32_t anakin_learn_static(anakin_t* h)
 extern "C" int32_t anakin_set_policy_gradient(anakin_t* h, int32_t kind)
 {
     NEED(h);
-    if (kind != ANAKIN_PG_SCORE_FUNCTION && kind != ANAKIN_PG_PATHWISE) { h->err = "unknown policy-gradient kind"; return ANAKIN_E_INVALID_ARG; }
+    if (kind < ANAKIN_PG_SCORE_FUNCTION || kind > ANAKIN_PG_PREFERENCE) { h->err = "unknown policy-gradient kind"; return ANAKIN_E_INVALID_ARG; }
     if (kind == ANAKIN_PG_PATHWISE && !pathwise_ok(h)) {
         h->err = "the pathwise policy gradient needs the pendulum with the tanh-Gaussian policy, an fp32 net of two equal hidden layers of 64, 128 or 256 units, and B a multiple of 16";
         return ANAKIN_E_BAD_CONFIG;
     }
+    if (kind >= ANAKIN_PG_CLIPPED && h->net.policy != POLICY_CATEGORICAL) {
+        h->err = "the clipped and the preference loss need a categorical policy";
+        return ANAKIN_E_BAD_CONFIG;
+    }
     h->pathwise = kind == ANAKIN_PG_PATHWISE ? 1 : 0;
+    h->token_loss = kind >= ANAKIN_PG_CLIPPED ? kind : 0;
+    return ANAKIN_OK;
+}
+
+extern "C" int32_t anakin_set_clip(anakin_t* h, double clip_low, double clip_high, double kl_coef)
+{
+    NEED(h);
+    if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !isfinite(clip_high) || !isfinite(kl_coef)) {
+        h->err = "clip_low has to lie in [0, 1], clip_high not below 0, kl_coef has to be finite";
+        return ANAKIN_E_INVALID_ARG;
+    }
+    h->clip_low = clip_low; h->clip_high = clip_high; h->kl_coef = kl_coef;
+    return ANAKIN_OK;
+}
+
+extern "C" int32_t anakin_set_preference(anakin_t* h, double beta, const float* d_label, const float* d_weight, int32_t chunks)
+{
+    NEED(h);
+    if (!isfinite(beta)) { h->err = "beta has to be finite"; return ANAKIN_E_INVALID_ARG; }
+    if ((d_label || d_weight) && chunks < 1) { h->err = "labels and weights need a row for every update"; return ANAKIN_E_INVALID_ARG; }
+    if (((uintptr_t)d_label | (uintptr_t)d_weight) & 3u) { h->err = "labels and weights have to be aligned to their type"; return ANAKIN_E_MISALIGNED; }
+    h->beta = beta; h->pair_label = d_label; h->pair_weight = d_weight; h->pair_chunks = chunks;
     return ANAKIN_OK;
 }
 
@@ -860,7 +945,7 @@ extern "C" int32_t anakin_step_decoupled(anakin_t* h)
 {
     NEED(h);
     if (h->n_updates != 1) { h->err = "decoupled steps apply one update per unroll"; return ANAKIN_E_BAD_CONFIG; }
-    if (h->pathwise) { h->err = "decoupled steps use the score-function gradient"; return ANAKIN_E_BAD_CONFIG; }
+    if (h->pathwise || h->token_loss) { h->err = "decoupled steps use the score-function gradient"; return ANAKIN_E_BAD_CONFIG; }
     if (h->prof_pending.size() > 8192) HIPCHK(h, prof_resolve(h));
     if (!h->actor_stream) {
         // no stream given by the caller (anakin_set_actor_stream): one of the library's own, default priority
@@ -896,6 +981,7 @@ extern "C" int32_t anakin_step_decoupled(anakin_t* h)
         HIPCHK(h, mc ? launch_replay_bf16(h, true) : launch_replay_forward(h, true));
         HIPCHK(h, launch_vtrace_loss(h));
         const int no_acts = h->traj_no_acts;
+        h->metric_token = 0;
         h->traj_packed = mc ? 1 : 0; h->traj_no_acts = one_layer_fused(h) ? 1 : 0;
         const int32_t r = run_update(h, true);
         h->traj_no_acts = no_acts;
@@ -1069,6 +1155,19 @@ extern "C" int32_t anakin_get_metrics(anakin_t* h, anakin_metrics* out)
     for (int b = 0; b < blocks; ++b) for (int k = 0; k < 5; ++k) s[k] += (double)part[(size_t)b * 8 + k];
     const double M = (double)h->B * h->T;
     out->policy_loss = s[0] / M; out->value_loss = s[1] / M; out->entropy_loss = s[2] / M;
+    if (h->metric_token) {
+        // the policy's terms are the operator's statistics, a mean over each chunk
+        std::vector<float> st((size_t)h->metric_chunks * 8);
+        rc = download(h, st.data(), h->lay.tok_stats, st.size() * 4);
+        if (rc) return rc;
+        double policy = 0.0, entropy = 0.0;
+        for (int k = 0; k < h->metric_chunks; ++k) {
+            const float* v = st.data() + (size_t)k * 8;
+            if (h->metric_token == ANAKIN_PG_CLIPPED) { policy += (double)v[1] + h->kl_coef * (double)v[2]; entropy -= (double)h->net_cfg.entropy_coef * (double)v[3]; }
+            else policy += (double)v[0];
+        }
+        out->policy_loss = policy / h->metric_chunks; out->entropy_loss = entropy / h->metric_chunks;
+    }
     out->loss = out->policy_loss + out->value_loss + out->entropy_loss;
     out->reward_sum = s[3];
     out->episodes = (int64_t)llround(s[4]);

@@ -152,6 +152,7 @@ struct Layout {
     size_t head_old;              // set while the loss is taken at a repeated forward pass: head outputs at acting time (0: none)
     size_t small_part;           // single-launch update of small nets: one whole gradient per workgroup, [workgroups][P]
     size_t counters;             // arrival counters of kernels whose last workgroup finishes the job (zero between launches)
+    size_t tok_ws, tok_stats, tok_label;   // token losses (clipped, preference): workspace (0: in dz[0]), statistics [T][8], labels of pairs [B/2]
     size_t path;                 // pathwise policy gradient: dL_path / d(mu, log_sigma) per sample, [T*B][2]
     size_t total;
 };
@@ -192,6 +193,11 @@ struct anakin {
     int bf16_path;                // the bf16 matrix-core kernels support this net
     int traj_packed;              // the stored unroll holds packed bf16 activations
     int traj_no_acts;             // the stored unroll holds no hidden activations (one-layer nets)
+    int token_loss;               // policy term by an operator of token policies: ANAKIN_PG_CLIPPED or ANAKIN_PG_PREFERENCE, else 0
+    double clip_low, clip_high, kl_coef, beta;   // their coefficients
+    const float *pair_label, *pair_weight;       // ANAKIN_PG_PREFERENCE: the caller's, [pair_chunks][B/2] (labels null: by the rewards)
+    int pair_chunks;
+    int metric_token, metric_chunks;             // the last update's kind and number of chunks, for the metrics
     int pathwise;                 // policy gradient through the environment instead of the score function (pendulum)
     int traj_decoupled;           // the stored unroll was collected by a decoupled step: behaviour parameters, no activations
     hipStream_t actor_stream;     // decoupled steps: the actor's stream (the caller's, or created on first use), and the fork/join events
@@ -245,6 +251,7 @@ bool scan_loss_ok(const anakin* h);          // returns and loss as one launch
 hipError_t launch_scan_loss(anakin* h, bool vtrace);
 hipError_t launch_vtrace_loss(anakin* h);
 hipError_t launch_head_grad(anakin* h);
+hipError_t launch_segment_labels(anakin* h, float* label);
 hipError_t launch_backward(anakin* h);
 hipError_t launch_adam(anakin* h);
 hipError_t launch_first_layer_grad(anakin* h);

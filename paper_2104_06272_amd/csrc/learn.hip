@@ -183,7 +183,9 @@ __device__ __forceinline__ HeadIn head_in(const HeadGradArgs& a, const int i)
     return x;
 }
 
-// one sample: its loss terms, and its head gradient to a.dhead.  A_, G_: advantage and return of the sample
+// one sample: its loss terms, and its head gradient to a.dhead.  A_, G_: advantage and return of the sample.  VALUES: the
+// value's part alone (the other columns get zeros: an operator of token policies fills them in)
+template <bool VALUES = false>
 __device__ __forceinline__ void head_grad_sample(const HeadGradArgs& a, const int i, const HeadIn& x, float A_, const float G_,
                                                  float& lp_term, float& v_term, float& e_term, float& rsum, float& dcount)
 {
@@ -197,7 +199,9 @@ __device__ __forceinline__ void head_grad_sample(const HeadGradArgs& a, const in
         const float dv = G_ - V;
         v_term = a.cv * dv * dv;
         const float gV = -2.0f * a.cv * dv * a.inv_m;
-        if (a.policy == POLICY_CATEGORICAL) {
+        if (VALUES) {
+            lp_term = 0.0f; e_term = 0.0f;
+        } else if (a.policy == POLICY_CATEGORICAL) {
             const int act = x.act;
             float mx = hv[0];
 #pragma unroll
@@ -266,13 +270,14 @@ __device__ __forceinline__ void loss_block_sums(float lp_term, float v_term, flo
     }
 }
 
+template <bool VALUES>
 __global__ __launch_bounds__(WG) void head_grad(const HeadGradArgs a, const SplitWeightsArgs sw, const int blocks)
 {
     if ((int)blockIdx.x >= blocks) { split_weights(sw, (int)blockIdx.x - blocks); return; }
     __shared__ float red[WG / 64][8];
     const int i = blockIdx.x * WG + threadIdx.x;
     float lp_term = 0.0f, v_term = 0.0f, e_term = 0.0f, rsum = 0.0f, dcount = 0.0f;
-    if (i < a.M) head_grad_sample(a, i, head_in(a, i), a.adv[i], a.ret[i], lp_term, v_term, e_term, rsum, dcount);
+    if (i < a.M) head_grad_sample<VALUES>(a, i, head_in(a, i), a.adv[i], a.ret[i], lp_term, v_term, e_term, rsum, dcount);
     loss_block_sums(lp_term, v_term, e_term, rsum, dcount, red, a.loss_part);
 }
 
@@ -943,7 +948,7 @@ bool catch_fused_ok(const anakin* h)
 {
     const NetShape& n = h->net;
     return one_layer_fused(h) && catch_fused_groups(n, h->env, h->B, h->T) > 0 && h->env.rows >= 2 && n.NH == 4 && h->n_updates == 1 &&
-           !h->traj_decoupled && !h->pathwise &&
+           !h->traj_decoupled && !h->pathwise && !h->token_loss &&
            n.dims[0] * CF_H * 4 < 65536 && n.w_off[0] % 4 == 0;           // board-cell offsets are packed into 16 bits; W1 is read 16 bytes at a time
 }
 
@@ -1222,7 +1227,25 @@ hipError_t launch_head_grad(anakin* h)
     h->metric_blocks = h->loss_blocks;
     const SplitWeightsArgs sw = split_weights_args(h);
     ProfScope prof(h, "head_grad");
-    hipLaunchKernelGGL(head_grad, dim3(h->loss_blocks + split_weights_blocks(sw)), dim3(WG), 0, h->stream, a, sw, h->loss_blocks);
+    hipLaunchKernelGGL(h->token_loss ? head_grad<true> : head_grad<false>, dim3(h->loss_blocks + split_weights_blocks(sw)), dim3(WG), 0, h->stream, a, sw, h->loss_blocks);
+    return hipGetLastError();
+}
+
+// Which environment of a pair (b, b + B / 2) had the larger sum of rewards over the steps the handle describes: 1 the first, 0
+// the second, 1/2 neither.  A lane per pair, sums in 64 bits and in the steps' order.
+__global__ __launch_bounds__(WG) void segment_labels(const int B, const int T, const float* __restrict__ rew, float* __restrict__ label)
+{
+    const int b = blockIdx.x * WG + threadIdx.x;
+    if (b >= B / 2) return;
+    double first = 0.0, second = 0.0;
+#pragma unroll 4
+    for (int t = 0; t < T; ++t) { first += (double)rew[(size_t)t * B + b]; second += (double)rew[(size_t)t * B + b + B / 2]; }
+    label[b] = first > second ? 1.0f : first < second ? 0.0f : 0.5f;
+}
+hipError_t launch_segment_labels(anakin* h, float* label)
+{
+    ProfScope prof(h, "segment_labels");
+    hipLaunchKernelGGL(segment_labels, dim3((h->B / 2 + WG - 1) / WG), dim3(WG), 0, h->stream, h->B, h->T, at<const float>(h, h->lay.tr_rew), label);
     return hipGetLastError();
 }
 
@@ -1237,7 +1260,7 @@ static bool scan_loss_shape(const anakin* h)
            h->B / E <= h->loss_blocks;
 }
 
-bool scan_loss_ok(const anakin* h) { return h->n_updates == 1 && !h->pathwise && !h->traj_decoupled && scan_loss_shape(h); }
+bool scan_loss_ok(const anakin* h) { return h->n_updates == 1 && !h->pathwise && !h->token_loss && !h->traj_decoupled && scan_loss_shape(h); }
 
 static void fill_vtrace_args(anakin* h, VtraceArgs& a)
 {

@@ -432,7 +432,7 @@ size_t small_fused_part_bytes(const EnvDims& ed, const NetShape& ns, int B, int 
 bool small_fused_ok(const anakin* h)
 {
     return small_fused_envs(h->env, h->net, h->B, h->T) > 0 && h->mode == 0 && h->n_updates == 1 && !h->traj_decoupled &&
-           !h->pathwise && !h->traj_packed && !h->traj_no_acts;
+           !h->pathwise && !h->token_loss && !h->traj_packed && !h->traj_no_acts;
 }
 
 hipError_t launch_learn_small_fused(anakin* h)

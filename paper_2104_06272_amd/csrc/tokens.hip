@@ -894,7 +894,7 @@ extern "C" int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, fl
 {
     SumArgs a{};
     TRY(check_rows(x, a.r));
-    if (x->rows > 0 && (!d_logp || !d_lse)) return fail(ANAKIN_E_INVALID_ARG, "null logp or lse");
+    if (x->rows > 0 && !d_logp) return fail(ANAKIN_E_INVALID_ARG, "null logp");
     a.logp = d_logp; a.lse = d_lse; a.entropy = d_entropy;
     LAUNCH(launch_sums(x->type, a, false, static_cast<hipStream_t>(hip_stream)));
     return ANAKIN_OK;

@@ -1,0 +1,264 @@
+"""Updates of an agent whose policy term comes from an operator of token policies: the clipped loss and the loss over pairs
+of environments, through anakin_learn, against the score-function update where the two agree and against a binary64
+statement of the whole update (forward pass, loss, gradient by automatic differentiation, Adam) where they do not."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import parity as PT
+from paper_2104_06272_amd import binding, workloads as W
+
+gpu = pytest.mark.gpu
+
+
+def _cfg(name, hidden=None, dtype=None, rows=None, cols=None, lr=None, **kw):
+    cfg = W.get(name, **{k: v for k, v in kw.items() if k in ("B", "T")})
+    cfg["env"] = dict(cfg["env"])
+    if hidden is not None:
+        cfg["net"]["hidden"] = list(hidden)
+    if dtype is not None:
+        cfg["net"]["dtype"] = dtype
+    if rows is not None:
+        cfg["env"].update(rows=rows, cols=cols)
+    if lr is not None:
+        cfg["net"]["lr"] = lr
+    return cfg
+
+
+def test_null_handles_are_refused():
+    L = binding.load()
+    assert L.anakin_set_clip(None, 0.2, 0.2, 0.0) == binding.E_INVALID_ARG
+    assert L.anakin_set_preference(None, 0.1, None, None, 0) == binding.E_INVALID_ARG
+
+
+SAME = [_cfg("catch_small"), _cfg("catch_4096", B=256), _cfg("catch_262144", B=512), _cfg("catch_4096", hidden=[256], B=64, T=7), _cfg("catch_4096", hidden=[128, 64, 32], B=64, T=5),
+        _cfg("maze_16384", hidden=[128, 128], B=64, T=8), _cfg("maze_16384", hidden=[256, 256], B=64, T=8), _cfg("maze_16384", hidden=[64, 64], dtype="fp32", rows=5, cols=7, B=32, T=6)]
+
+
+@gpu
+@pytest.mark.parametrize("cfg", SAME, ids=lambda c: f"{c['name']}-{'-'.join(map(str, c['net']['hidden']))}-{c['net']['dtype']}")
+def test_clipped_update_at_the_acting_parameters_is_the_score_functions(cfg):
+    """The ratio is 1 there: same gradient, so same parameters, whatever kernels the plain update fuses; the KL term has no
+    gradient at its minimum."""
+    a, b = binding.Anakin(cfg, seed=2), binding.Anakin(cfg, seed=2)
+    b.set_policy_gradient(binding.PG_CLIPPED)
+    b.set_clip(0.1, 0.3, 0.5)
+    tol = 2e-2 if cfg["net"]["dtype"] == "bf16" else 1e-4
+    regions, _ = PT.param_regions(cfg)
+    for step in range(2):
+        b.set_params(a.get_params())
+        b.set_opt_state(*a.get_opt_state())
+        a.rollout(); b.rollout()
+        a.learn(); b.learn()
+        PT.assert_regions_close("gradient", b.get_grads(), a.get_grads(), regions, tol)
+        ma, mb, tr = a.metrics(), b.metrics(), b.trajectory()
+        assert abs(mb["value_loss"] - ma["value_loss"]) <= 1e-5 * abs(ma["value_loss"]) + 1e-9
+        assert abs(mb["entropy_loss"] - ma["entropy_loss"]) <= 1e-5 * abs(ma["entropy_loss"])
+        adv = tr["adv"].astype(np.float64)
+        assert abs(mb["policy_loss"] + adv.mean()) <= 1e-5 * np.abs(adv).mean()
+        assert mb["reward_sum"] == ma["reward_sum"] and mb["episodes"] == ma["episodes"]
+    # back to the score function: the plain update again, and its metrics
+    b.set_policy_gradient(binding.PG_SCORE_FUNCTION)
+    b.set_params(a.get_params()); b.set_opt_state(*a.get_opt_state())
+    a.rollout(); b.rollout(); a.learn(); b.learn()
+    assert np.array_equal(a.get_params(), b.get_params()) and a.metrics() == b.metrics()
+    a.close(); b.close()
+
+
+def _forward(cfg, theta, x):
+    """head outputs and nothing rounded: theta a flat binary64 tensor"""
+    dims = [x.shape[1]] + list(cfg["net"]["hidden"])
+    off = 0
+    for k, n in zip(dims[:-1], dims[1:]):
+        w, b = theta[off:off + k * n].view(k, n), theta[off + k * n:off + k * n + n]
+        off += k * n + n
+        x = torch.relu(x @ w + b)
+    nh = (theta.numel() - off) // (dims[-1] + 1)
+    return x @ theta[off:off + dims[-1] * nh].view(dims[-1], nh) + theta[off + dims[-1] * nh:]
+
+
+def _reference(cfg, tr, theta, m, v, t, updates, policy_term):
+    """N sequential updates in binary64; returns last gradient, parameters, and the chunks' losses.  policy_term(logp, logp_old,
+    log p, chunk) -> (policy loss, entropy loss)"""
+    net = {k: float(np.float32(x)) for k, x in cfg["net"].items() if isinstance(x, float)}
+    T, B = tr["reward"].shape
+    x = torch.tensor(PT.np_observation(cfg, tr))
+    act = torch.tensor(tr["action"].astype(np.int64).ravel())
+    ret = torch.tensor(tr["ret"].astype(np.float64).ravel())
+    theta, m, v = torch.tensor(theta.astype(np.float64)), m.astype(np.float64), v.astype(np.float64)
+    old = torch.log_softmax(_forward(cfg, theta, x)[:, :-1], 1).gather(1, act[:, None]).reshape(-1)
+    losses, n = [], T // updates * B
+    for k in range(updates):
+        s = slice(k * n, (k + 1) * n)
+        th = theta.clone().requires_grad_(True)
+        head = _forward(cfg, th, x[s])
+        logs = torch.log_softmax(head[:, :-1], 1)
+        policy, entropy = policy_term(logs.gather(1, act[s, None]).reshape(-1), old[s], logs, k, s)
+        value = net["value_coef"] * ((ret[s] - head[:, -1]) ** 2).mean()
+        (policy + entropy + value).backward()
+        g = th.grad.numpy()
+        t += 1
+        m = net["beta1"] * m + (1 - net["beta1"]) * g
+        v = net["beta2"] * v + (1 - net["beta2"]) * g * g
+        step = net["lr"] * (m / (1 - net["beta1"] ** t)) / (np.sqrt(v / (1 - net["beta2"] ** t)) + net["eps"])
+        theta = theta - torch.tensor(step)
+        losses.append([float(policy.detach()), float(value.detach()), float(entropy.detach())])
+    return g, theta.numpy(), np.array(losses).mean(0)
+
+
+def _warm(cfg, seed, steps=6):
+    g = binding.Anakin(cfg, seed=seed)
+    for _ in range(steps):
+        g.step()
+    g.rollout()
+    return g, g.get_params(), g.get_opt_state()
+
+
+def _check(g, cfg, start, updates, term):
+    theta, (m, v, t) = start
+    tr = g.trajectory()
+    grad, params, losses = _reference(cfg, tr, theta, m, v, t, updates, lambda *a: term(tr, *a))
+    regions, _ = PT.param_regions(cfg)
+    # the parameters a second update starts from carry the first one's roundings (Adam divides by sqrt(v): 1e-6 of a step)
+    PT.assert_regions_close("gradient", g.get_grads(), grad, regions, 1e-4 if updates == 1 else 1e-3)
+    assert PT.rel(g.get_params() - theta, params - theta) <= (1e-4 if updates == 1 else 1e-3)
+    got = g.metrics()
+    for name, want in zip(("policy_loss", "value_loss", "entropy_loss"), losses):
+        assert abs(got[name] - want) <= 1e-4 * max(abs(want), 1e-2), (name, got[name], want)
+
+
+@gpu
+@pytest.mark.parametrize("updates,kl", [(1, 0.0), (2, 0.0), (4, 0.3)])
+@pytest.mark.parametrize("hidden", [[64, 64], [32], [256, 128]])
+def test_clipped_updates_follow_the_reference(hidden, updates, kl):
+    cfg = _cfg("catch_small", hidden=hidden, B=64, T=20, lr=0.01)
+    g, theta, opt = _warm(cfg, seed=5)
+    g.set_policy_gradient(binding.PG_CLIPPED)
+    g.set_clip(0.05, 0.08, kl)
+    g.set_updates_per_unroll(updates, sequential=True)
+    g.learn()
+    ent = float(np.float32(cfg["net"]["entropy_coef"]))
+    clipped = []
+
+    def term(tr, lp, old, logs, k, s):
+        adv = torch.tensor(tr["adv"].astype(np.float64).ravel())[s]
+        r = torch.exp(lp - old)
+        d = old - lp
+        clipped.append(float(((r * adv) > r.clamp(0.95, 1.08) * adv).double().mean()))
+        return -torch.minimum(r * adv, r.clamp(0.95, 1.08) * adv).mean() + kl * (torch.exp(d) - d - 1).mean(), ent * (torch.exp(logs) * logs).sum(1).mean()
+    _check(g, cfg, (theta, opt), updates, term)
+    assert clipped[0] == 0.0 and (updates == 1 or max(clipped) > 0.0)          # the case clips
+    g.close()
+
+
+@gpu
+@pytest.mark.parametrize("updates", [1, 2])
+@pytest.mark.parametrize("given", [False, True])
+def test_preference_updates_follow_the_reference(updates, given):
+    cfg = _cfg("catch_small", hidden=[64, 64], B=64, T=20, lr=0.01)
+    B = 64
+    g, theta, opt = _warm(cfg, seed=7)
+    g.set_policy_gradient(binding.PG_PREFERENCE)
+    gen = torch.Generator().manual_seed(1)
+    label, weight = torch.rand(updates, B // 2, generator=gen), torch.rand(updates, B // 2, generator=gen) * (torch.arange(B // 2) % 4 != 2)
+    if given:
+        g.set_preference(0.4, label.cuda(), weight.cuda())
+    else:
+        g.set_preference(0.4)
+    g.set_updates_per_unroll(updates, sequential=True)
+    g.learn()
+
+    def term(tr, lp, old, logs, k, s):
+        d = (lp - old).view(-1, B).sum(0)
+        h = 0.4 * (d[:B // 2] - d[B // 2:])
+        rew = torch.tensor(tr["reward"].astype(np.float64).ravel())[s].view(-1, B).sum(0)
+        y = label[k].double() if given else 0.5 + 0.5 * torch.sign(rew[:B // 2] - rew[B // 2:])
+        w = weight[k].double() if given else torch.ones(B // 2).double()
+        loss = -(y * torch.nn.functional.logsigmoid(h) + (1 - y) * torch.nn.functional.logsigmoid(-h))
+        return (w * loss).sum() / w.sum(), torch.zeros((), dtype=torch.float64)
+    _check(g, cfg, (theta, opt), updates, term)
+    g.close()
+
+
+@gpu
+@pytest.mark.parametrize("kind", [binding.PG_CLIPPED, binding.PG_PREFERENCE])
+def test_static_scratch_gives_the_same_update(kind):
+    for cfg, updates in ((_cfg("catch_4096", B=256, T=8), 2), (_cfg("catch_small", B=16, T=4), 1), (_cfg("maze_16384", hidden=[256, 256], B=64, T=8), 2)):
+        a, b = binding.Anakin(cfg, seed=3), binding.Anakin(cfg, seed=3)
+        for g in (a, b):
+            g.set_policy_gradient(kind)
+            g.set_updates_per_unroll(updates, sequential=True)
+        a.rollout(); a.learn(); b.rollout(); b.learn_static()
+        assert np.array_equal(a.get_params(), b.get_params()) and a.metrics() == b.metrics()
+        assert np.abs(a.get_grads()).max() > 0
+        a.close(); b.close()
+
+
+@gpu
+def test_captured_update_replays():
+    """anakin_learn with the clipped loss in a graph: every replay is the eager update of the same stored unroll."""
+    cfg = _cfg("catch_4096", B=64, T=8)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        g = binding.Anakin(cfg, seed=1, stream=side)
+        g.set_policy_gradient(binding.PG_CLIPPED)
+        g.step()
+        g.rollout()
+        torch.cuda.synchronize()
+        start = g.ws.clone()
+        g.learn()
+        torch.cuda.synchronize()
+        want, grads = g.get_params(), g.get_grads()
+        opt = g.get_opt_state()
+        g.ws.copy_(start)
+        g.set_opt_state(*[x if i < 2 else opt[2] - 1 for i, x in enumerate(g.get_opt_state())])
+        g.rollout()                                               # (the handle wants a stored unroll before it learns; it is the next one,
+        torch.cuda.synchronize()                                  #  and is put back below)
+        graph = torch.cuda.CUDAGraph()
+        g.ws.copy_(start)
+        with torch.cuda.graph(graph, stream=side):
+            g.learn()
+    for k in range(3):
+        with torch.cuda.stream(side):
+            g.ws.copy_(start)
+            graph.replay()
+            side.synchronize()
+        assert np.array_equal(g.get_grads(), grads) and np.array_equal(g.get_params(), want), k
+    g.close()
+
+
+@gpu
+def test_refusals():
+    g = binding.Anakin(_cfg("pendulum_8192", hidden=[64, 64], B=64, T=4), seed=0)
+    for kind in (binding.PG_CLIPPED, binding.PG_PREFERENCE):
+        with pytest.raises(binding.AnakinError) as e:
+            g.set_policy_gradient(kind)
+        assert e.value.code == binding.E_BAD_CONFIG
+    g.close()
+    g = binding.Anakin(_cfg("catch_small"), seed=0)
+    for bad in ((-0.1, 0.2, 0.0), (1.1, 0.2, 0.0), (0.2, -0.2, 0.0), (0.2, float("inf"), 0.0), (0.2, 0.2, float("nan"))):
+        with pytest.raises(binding.AnakinError):
+            g.set_clip(*bad)
+    with pytest.raises(binding.AnakinError):
+        g.set_policy_gradient(4)
+    with pytest.raises(binding.AnakinError):
+        g.set_preference(float("nan"))
+    with pytest.raises(binding.AnakinError):
+        g.set_preference(0.1, torch.zeros(1, 31, device="cuda"))
+    with pytest.raises(binding.AnakinError):
+        g.set_preference(0.1, torch.zeros(1, 32))
+    g.set_policy_gradient(binding.PG_PREFERENCE)
+    g.set_preference(0.1, torch.zeros(1, 32, device="cuda"))
+    g.set_updates_per_unroll(2)
+    g.rollout()
+    with pytest.raises(binding.AnakinError) as e:
+        g.learn()                                                 # two updates, one row of labels
+    assert e.value.code == binding.E_STATE
+    g.set_updates_per_unroll(1)
+    g.learn()
+    with pytest.raises(binding.AnakinError) as e:
+        g.step_decoupled()
+    assert e.value.code == binding.E_BAD_CONFIG
+    g.close()
