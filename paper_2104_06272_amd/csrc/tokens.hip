@@ -257,8 +257,8 @@ __device__ __forceinline__ int policy_target(const PolicyArgs& a, int64_t n)
 }
 
 // ---------------------------------------------------------------------------
-// Short rows.  `lanes` lanes (a power of two up to 64) hold a row, NE elements each: VECTOR -- 16 bytes at a time, piece k of
-// lane l at vector k lanes + l; else one element at a time, element k of lane l in column k lanes + l.  Everything of a row
+// Short rows.  `lanes` lanes (a power of two up to 64) hold a row: PIECES of 16 bytes each, piece k lanes + l at lane l, and a
+// loose element; or (PIECES 0) four single elements, element k of lane l in column k lanes + l.  Everything of a row
 // happens in registers; all its lanes carry out the row's 64-bit arithmetic together.
 // ---------------------------------------------------------------------------
 enum { DO_SUMS, DO_GRADIENT, DO_POLICY };
@@ -267,55 +267,47 @@ template <> struct LaneArgs<DO_SUMS> { SumArgs s; int lanes; __device__ const Ro
 template <> struct LaneArgs<DO_GRADIENT> { GradArgs g; int lanes; __device__ const Rows& rows() const { return g.r; } };
 template <> struct LaneArgs<DO_POLICY> { PolicyArgs p; int lanes; __device__ const Rows& rows() const { return p.r; } };
 
-template <class E, int NE, bool VECTOR>
+template <class E, int PIECES>
 struct LaneRow {
     typedef typename E::T T;
-    static __device__ __forceinline__ void load(const T* row, int V, int lanes, int l, float (&z)[NE])
+    static constexpr bool VECTOR = PIECES > 0;
+    static constexpr int NE = VECTOR ? PIECES * E::N + 1 : 4;           // VECTOR: the last one is loose
+    static __device__ __forceinline__ void load(const T* row, const Cut& cut, int V, int lanes, int l, float (&z)[NE])
     {
-        if (VECTOR) {
+        if constexpr (VECTOR) {
 #pragma unroll
-            for (int k = 0; k < NE / E::N; ++k) {
-                const int j = (k * lanes + l) * E::N;
-                if (j + E::N <= V) {
-                    float f[E::N];
-                    E::unpack(*reinterpret_cast<const u32x4_any*>(row + j), f);
+            for (int k = 0; k < PIECES; ++k) {
+                const int v = k * lanes + l;
+                float f[E::N];
+                if (v < cut.pieces) E::unpack(*reinterpret_cast<const u32x4_any*>(row + cut.head + v * E::N), f);
 #pragma unroll
-                    for (int i = 0; i < E::N; ++i) z[k * E::N + i] = f[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < E::N; ++i) z[k * E::N + i] = j + i < V ? E::get(row + j + i) : -INFINITY;
-                }
+                for (int i = 0; i < E::N; ++i) z[k * E::N + i] = v < cut.pieces ? f[i] : -INFINITY;
             }
+            z[NE - 1] = l < cut.loose ? E::get(row + loose_column<E>(cut, l)) : -INFINITY;
         } else {
 #pragma unroll
             for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; z[k] = j < V ? E::get(row + j) : -INFINITY; }
         }
     }
-    // the gradient d, and `more` at column `target`; d null (zero): zeros
-    static __device__ __forceinline__ void store(T* out, int V, int lanes, int l, float (&d)[NE], int target, float more)
+    // the gradient d, and `more` at column `target`
+    static __device__ __forceinline__ void store(T* out, const Cut& cut, int V, int lanes, int l, float (&d)[NE], int target, float more)
     {
+        if constexpr (VECTOR) {
+            const int tv = target >= cut.head ? (target - cut.head) / E::N : -1, ti = (target - cut.head) % E::N;
 #pragma unroll
-        for (int k = 0; k < NE; ++k) {
-            const int j = VECTOR ? ((k / E::N) * lanes + l) * E::N + k % E::N : k * lanes + l;
-            d[k] += j == target ? more : 0.0f;
-        }
-        if (VECTOR) {
-#pragma unroll
-            for (int k = 0; k < NE / E::N; ++k) {
-                const int j = (k * lanes + l) * E::N;
-                if (j + E::N <= V) {
+            for (int k = 0; k < PIECES; ++k) {
+                const int v = k * lanes + l;
+                if (v < cut.pieces) {
                     float f[E::N];
 #pragma unroll
-                    for (int i = 0; i < E::N; ++i) f[i] = d[k * E::N + i];
-                    *reinterpret_cast<u32x4_any*>(out + j) = E::pack(f);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < E::N; ++i) if (j + i < V) E::put(out + j + i, d[k * E::N + i]);
+                    for (int i = 0; i < E::N; ++i) f[i] = d[k * E::N + i] + (v == tv && i == ti ? more : 0.0f);
+                    *reinterpret_cast<u32x4_any*>(out + cut.head + v * E::N) = E::pack(f);
                 }
             }
+            if (l < cut.loose) { const int j = loose_column<E>(cut, l); E::put(out + j, d[NE - 1] + (j == target ? more : 0.0f)); }
         } else {
 #pragma unroll
-            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; if (j < V) E::put(out + j, d[k]); }
+            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; if (j < V) E::put(out + j, d[k] + (j == target ? more : 0.0f)); }
         }
     }
 };
@@ -335,11 +327,12 @@ __device__ __forceinline__ Sums lanes_part(const float (&z)[NE], const Rows& r, 
     return Sums{m, (double)p.s, (double)p.u};
 }
 
-template <class E, int DO, int NE, bool VECTOR, bool FINE>
+template <class E, int DO, int PIECES, bool FINE>
 __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
 {
     typedef typename E::T T;
-    typedef LaneRow<E, NE, VECTOR> L;
+    typedef LaneRow<E, PIECES> L;
+    constexpr int NE = L::NE;
     __shared__ FinishLds lds;
     const Rows& r = a.rows();
     const int lanes = a.lanes, l = threadIdx.x & (lanes - 1), per = WG / lanes, V = r.V;
@@ -363,19 +356,22 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
             if (!there) continue;
             const RowGrad q = grad_of_row(a.g, n);
             target = q.target;
-            if (target >= 0) { L::load(row, V, lanes, l, z); gradient_of<true>(q, z, d); }
+            T* out = static_cast<T*>(a.g.out) + n * a.g.out_stride;
+            const Cut cut = cut_at<E>(row, V);
+            if (target >= 0) { L::load(row, cut, V, lanes, l, z); gradient_of<true>(q, z, d); }
             else {
 #pragma unroll
                 for (int k = 0; k < NE; ++k) d[k] = 0.0f;
             }
-            L::store(static_cast<T*>(a.g.out) + n * a.g.out_stride, V, lanes, l, d, target, q.to_target);
+            L::store(out, cut, V, lanes, l, d, target, q.to_target);
         } else {
         PolicyIn in{};
         if constexpr (DO == DO_POLICY) {
             if (there) target = policy_target(a.p, n);
             if (target >= 0) in = policy_in(a.p.p, n);
         } else if (there) target = row_target(r, n);
-        if (target >= 0) L::load(row, V, lanes, l, z);
+        const Cut cut = cut_at<E>(row, V);
+        if (target >= 0) L::load(row, cut, V, lanes, l, z);
         else {
 #pragma unroll
             for (int k = 0; k < NE; ++k) z[k] = 0.0f;
@@ -402,7 +398,7 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
 #pragma unroll
             for (int k = 0; k < NE; ++k) d[k] = 0.0f;
         }
-        L::store(static_cast<T*>(a.p.out) + n * a.p.out_stride, V, lanes, l, d, target, q.to_target);
+        L::store(static_cast<T*>(a.p.out) + n * a.p.out_stride, cut, V, lanes, l, d, target, q.to_target);
         }
         }
     }
@@ -450,13 +446,14 @@ __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
     Sums sums{};
     if (target >= 0) {
         constexpr int U = 4;                                            // loads in flight
-        const int vecs = V / E::N;
+        const Cut cut = cut_at<E>(row, V);
+        const typename E::T* in = row + cut.head;
         const float c = a.r.c, c_lo = a.r.c_lo;
         int v = threadIdx.x;
-        for (; v + (U - 1) * nt < vecs; v += U * nt) {
+        for (; v + (U - 1) * nt < cut.pieces; v += U * nt) {
             u32x4_any w[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(v + k * nt) * E::N);
+            for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * nt) * E::N);
             float z[U][E::N], m = p.m;
 #pragma unroll
             for (int k = 0; k < U; ++k) { E::unpack(w[k], z[k]); m = max_of(z[k], m); }
@@ -466,19 +463,52 @@ __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
 #pragma unroll
             for (int k = 0; k < U; ++k) add_at<FINE>(p, z[k], m0, s, c, c_lo);
         }
-        for (; v < vecs; v += nt) {
+        for (; v < cut.pieces; v += nt) {
             float z[E::N];
-            E::unpack(*reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N), z);
+            E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
             add_elements<FINE>(p, z, c, c_lo);
         }
-        const int j = vecs * E::N + threadIdx.x;
-        if (j < V) {
-            const float z[1] = {E::get(row + j)};
+        if ((int)threadIdx.x < cut.loose) {
+            const float z[1] = {E::get(row + loose_column<E>(cut, threadIdx.x))};
             add_elements<FINE>(p, z, c, c_lo);
         }
         sums = block_joined<FINE>(p, c, c_lo, lds, lds_s);
     }
     if (threadIdx.x == 0) store_sums<FINE>(a, n, sums, target, chosen);
+}
+
+// zeros in all of a row of the gradient
+template <class E, int NT>
+__device__ __forceinline__ void zero_row(typename E::T* out, int V)
+{
+    const Cut cut = cut_at<E>(out, V);
+    for (int v = threadIdx.x; v < cut.pieces; v += NT) *reinterpret_cast<u32x4_any*>(out + cut.head + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
+    if ((int)threadIdx.x < cut.loose) E::put(out + loose_column<E>(cut, threadIdx.x), 0.0f);
+}
+template <class E, bool ENT>
+__device__ __forceinline__ void put_piece(const RowGrad& q, const u32x4_any& w, typename E::T* out)
+{
+    float z[E::N], d[E::N];
+    E::unpack(w, z);
+    gradient_of<ENT>(q, z, d);
+    *reinterpret_cast<u32x4_any*>(out) = E::pack(d);
+}
+template <class E, bool ENT>
+__device__ __forceinline__ void put_element(const RowGrad& q, float x, float more, typename E::T* out)
+{
+    const float z[1] = {x};
+    float d[1];
+    gradient_of<ENT>(q, z, d);
+    E::put(out, d[0] + more);
+}
+// whether this thread stores column `target` of a row whose piece v goes to thread v % NT: it stores it once more behind its
+// pieces, with what the target gets beside the others (stores of one thread to one place keep their order)
+template <class E, int NT>
+__device__ __forceinline__ bool stores_target(const Cut& cut, int target)
+{
+    const int i = target - cut.head, v = i / E::N;
+    if (i < 0) return (int)threadIdx.x == target;
+    return v < cut.pieces ? (int)threadIdx.x == v % NT : (int)threadIdx.x == target - cut.pieces * E::N;
 }
 
 // ---------------------------------------------------------------------------
@@ -495,39 +525,23 @@ __global__ __launch_bounds__(WG) void block_gradients(const GradArgs a)
     const RowGrad q = grad_of_row(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
-    const int V = a.r.V, vecs = V / E::N;
-    if (q.target < 0) {
-        for (int v = threadIdx.x; v < vecs; v += WG) *reinterpret_cast<u32x4_any*>(out + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
-        for (int j = vecs * E::N + threadIdx.x; j < V; j += WG) E::put(out + j, 0.0f);
-        return;
-    }
+    if (q.target < 0) { zero_row<E, WG>(out, a.r.V); return; }
+    const Cut cut = cut_at<E>(row, a.r.V);
+    const float chosen = E::get(row + q.target);                        // (before it is overwritten)
+    const T* in = row + cut.head;
+    T* to = out + cut.head;
     constexpr int U = 4;
     int v = threadIdx.x;
-    const int tv = q.target / E::N;
-    auto piece = [&](int at, const u32x4_any& w) {
-        float z[E::N], d[E::N];
-        E::unpack(w, z);
-        gradient_of<ENT>(q, z, d);
-        if (at == tv) {
-#pragma unroll
-            for (int i = 0; i < E::N; ++i) d[i] += at * E::N + i == q.target ? q.to_target : 0.0f;
-        }
-        *reinterpret_cast<u32x4_any*>(out + (int64_t)at * E::N) = E::pack(d);
-    };
-    for (; v + (U - 1) * WG < vecs; v += U * WG) {
+    for (; v + (U - 1) * WG < cut.pieces; v += U * WG) {
         u32x4_any w[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(v + k * WG) * E::N);
+        for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * WG) * E::N);
 #pragma unroll
-        for (int k = 0; k < U; ++k) piece(v + k * WG, w[k]);
+        for (int k = 0; k < U; ++k) put_piece<E, ENT>(q, w[k], to + (int64_t)(v + k * WG) * E::N);
     }
-    for (; v < vecs; v += WG) piece(v, *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N));
-    const int j = vecs * E::N + threadIdx.x;
-    if (j < V) {
-        float z[1] = {E::get(row + j)}, d[1];
-        gradient_of<ENT>(q, z, d);
-        E::put(out + j, d[0] + (j == q.target ? q.to_target : 0.0f));
-    }
+    for (; v < cut.pieces; v += WG) put_piece<E, ENT>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
+    if ((int)threadIdx.x < cut.loose) { const int j = loose_column<E>(cut, threadIdx.x); put_element<E, ENT>(q, E::get(row + j), 0.0f, out + j); }
+    if (stores_target<E, WG>(cut, q.target)) put_element<E, ENT>(q, chosen, q.to_target, out + q.target);
 }
 
 // ---------------------------------------------------------------------------
@@ -543,15 +557,12 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
     __shared__ double weights[WAVES];
     __shared__ RowGrad row_grad;
     const int64_t n = blockIdx.x;
-    const int V = a.r.V, vecs = V / E::N, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int target = policy_target(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
     if (target < 0) {
-        if (a.out) {
-            for (int v = tid; v < vecs; v += NT) *reinterpret_cast<u32x4_any*>(out + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
-            for (int j = vecs * E::N + tid; j < V; j += NT) E::put(out + j, 0.0f);
-        }
+        if (a.out) zero_row<E, NT>(out, a.r.V);
         if (tid == 0) {
             if (a.logp) a.logp[n] = 0.0f;
 #pragma unroll
@@ -559,34 +570,36 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
         }
         return;
     }
+    const Cut cut = cut_at<E>(row, a.r.V);
+    const T* in = row + cut.head;
     // (loads return in order: the few small ones first)
-    PolicyIn in{};
-    if (tid == 0) in = policy_in(a.p, n);
+    PolicyIn pin{};
+    if (tid == 0) pin = policy_in(a.p, n);
     double share = weight_share(a.norm, a.r, tid, NT);
+    const float chosen = E::get(row + target);
     u32x4_any w[VPT];
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
-        if (tid + k * NT < vecs) w[k] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(tid + k * NT) * E::N);
-    const int j_tail = vecs * E::N + tid;
-    const float z_tail = j_tail < V ? E::get(row + j_tail) : -INFINITY;
-    const float chosen = E::get(row + target);
+        if (tid + k * NT < cut.pieces) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(tid + k * NT) * E::N);
+    const int j_loose = loose_column<E>(cut, tid);
+    const float z_loose = tid < cut.loose ? E::get(row + j_loose) : -INFINITY;
     share = wave_sum(share);
     // maximum of the wavefront's pieces, then their sums at that shift
     const float c = a.r.c, c_lo = a.r.c_lo;
-    float m = z_tail;
+    float m = z_loose;
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
-        if (tid + k * NT < vecs) { float z[E::N]; E::unpack(w[k], z); m = max_of(z, m); }
+        if (tid + k * NT < cut.pieces) { float z[E::N]; E::unpack(w[k], z); m = max_of(z, m); }
     for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     Part p{m, 0.0f, 0.0f};
     const Shift s = shift_of(m, c);
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
-        if (tid + k * NT < vecs) { float z[E::N]; E::unpack(w[k], z); add_at<false>(p, z, 0.0f, s, c, c_lo); }
-    if (j_tail < V) { const float z[1] = {z_tail}; add_at<false>(p, z, 0.0f, s, c, c_lo); }
-    for (int v = tid + VPT * NT; v < vecs; v += NT) {
+        if (tid + k * NT < cut.pieces) { float z[E::N]; E::unpack(w[k], z); add_at<false>(p, z, 0.0f, s, c, c_lo); }
+    if (tid < cut.loose) { const float z[1] = {z_loose}; add_at<false>(p, z, 0.0f, s, c, c_lo); }
+    for (int v = tid + VPT * NT; v < cut.pieces; v += NT) {
         float z[E::N];
-        E::unpack(*reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N), z);
+        E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
         add_elements<false>(p, z, c, c_lo);
     }
     p = lanes_joined<false>(p, c, c_lo, 64);
@@ -599,7 +612,7 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
         if (lane == 0) {
             const RowSum x = finish_row<false>(Sums{p.m, (double)p.s, (double)p.u}, a.r);
             const double lp = logp_of<false>(x, chosen, a.r), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
-            const PolicyRow y = policy_row(a.p, in, lp, x.entropy, x.empty);
+            const PolicyRow y = policy_row(a.p, pin, lp, x.entropy, x.empty);
             row_grad = row_gradient(x, y.g * inv, y.e * inv, target, a.r.scale);
             if (a.logp) a.logp[n] = (float)lp;
             double v[STATS] = {};
@@ -611,26 +624,13 @@ __global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
     if (!a.out) return;
     __syncthreads();
     const RowGrad q = row_grad;
-    const int tv = q.target / E::N;
-    auto piece = [&](int at, const u32x4_any& x) {
-        float z[E::N], d[E::N];
-        E::unpack(x, z);
-        gradient_of<ENT>(q, z, d);
-        if (at == tv) {
-#pragma unroll
-            for (int i = 0; i < E::N; ++i) d[i] += at * E::N + i == q.target ? q.to_target : 0.0f;
-        }
-        *reinterpret_cast<u32x4_any*>(out + (int64_t)at * E::N) = E::pack(d);
-    };
+    T* to = out + cut.head;
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
-        if (tid + k * NT < vecs) piece(tid + k * NT, w[k]);
-    for (int v = tid + VPT * NT; v < vecs; v += NT) piece(v, *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * E::N));
-    if (j_tail < V) {
-        float z[1] = {z_tail}, d[1];
-        gradient_of<ENT>(q, z, d);
-        E::put(out + j_tail, d[0] + (j_tail == q.target ? q.to_target : 0.0f));
-    }
+        if (tid + k * NT < cut.pieces) put_piece<E, ENT>(q, w[k], to + (int64_t)(tid + k * NT) * E::N);
+    for (int v = tid + VPT * NT; v < cut.pieces; v += NT) put_piece<E, ENT>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
+    if (tid < cut.loose) put_element<E, ENT>(q, z_loose, 0.0f, out + j_loose);
+    if (stores_target<E, NT>(cut, target)) put_element<E, ENT>(q, chosen, q.to_target, out + target);
 }
 
 // ---------------------------------------------------------------------------
@@ -799,7 +799,7 @@ static unsigned lane_grid(const LaneForm& f, int64_t rows)
 template <class E, int DO, bool FINE>
 static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid, hipStream_t s)
 {
-    auto k = f.pieces == 0 ? lanes_rows<E, DO, 4, false, FINE> : f.pieces == 1 ? lanes_rows<E, DO, E::N, true, FINE> : lanes_rows<E, DO, 4 * E::N, true, FINE>;
+    auto k = f.pieces == 0 ? lanes_rows<E, DO, 0, FINE> : f.pieces == 1 ? lanes_rows<E, DO, 1, FINE> : lanes_rows<E, DO, 4, FINE>;
     hipLaunchKernelGGL(k, dim3(grid), dim3(WG), 0, s, a);
 }
 #define BY_TYPE(type, f, ...) ((type) == ANAKIN_TYPE_FP32 ? f<Fp32, __VA_ARGS__> : (type) == ANAKIN_TYPE_BF16 ? f<Bf16, __VA_ARGS__> : f<Fp16, __VA_ARGS__>)
