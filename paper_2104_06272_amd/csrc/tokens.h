@@ -95,9 +95,9 @@ struct Fp16 {
 
 struct Cut { int head, pieces, loose; };         // loose: in front and behind, 14 at most
 template <class E>
-__device__ __forceinline__ Cut cut_at(const typename E::T* row, int V)
+__device__ __forceinline__ Cut cut_at(const typename E::T* row, int V, bool at_border = true)      // false: pieces from column 0 on
 {
-    int head = (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(typename E::T);
+    int head = at_border ? (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(typename E::T) : 0;
     head = head < V ? head : V;
     const int pieces = (V - head) / E::N;
     return Cut{head, pieces, V - pieces * E::N};

@@ -258,8 +258,9 @@ __device__ __forceinline__ int policy_target(const PolicyArgs& a, int64_t n)
 
 // ---------------------------------------------------------------------------
 // Short rows.  `lanes` lanes (a power of two up to 64) hold a row: PIECES of 16 bytes each, piece k lanes + l at lane l, and a
-// loose element; or (PIECES 0) four single elements, element k of lane l in column k lanes + l.  Everything of a row
-// happens in registers; all its lanes carry out the row's 64-bit arithmetic together.
+// loose element (8 lanes: pieces from column 0 on, which leaves no more than 7 loose); or (PIECES 0) four single elements, element
+// k of lane l in column k lanes + l.  Everything of a row happens in registers; all its lanes carry out the row's 64-bit
+// arithmetic together, so that a row should have few of them.
 // ---------------------------------------------------------------------------
 enum { DO_SUMS, DO_GRADIENT, DO_POLICY };
 template <int DO> struct LaneArgs;
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
             const RowGrad q = grad_of_row(a.g, n);
             target = q.target;
             T* out = static_cast<T*>(a.g.out) + n * a.g.out_stride;
-            const Cut cut = cut_at<E>(row, V);
+            const Cut cut = cut_at<E>(row, V, lanes >= 16);
             if (target >= 0) { L::load(row, cut, V, lanes, l, z); gradient_of<true>(q, z, d); }
             else {
 #pragma unroll
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
             if (there) target = policy_target(a.p, n);
             if (target >= 0) in = policy_in(a.p.p, n);
         } else if (there) target = row_target(r, n);
-        const Cut cut = cut_at<E>(row, V);
+        const Cut cut = cut_at<E>(row, V, lanes >= 16);
         if (target >= 0) L::load(row, cut, V, lanes, l, z);
         else {
 #pragma unroll
@@ -477,21 +478,24 @@ __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
     if (threadIdx.x == 0) store_sums<FINE>(a, n, sums, target, chosen);
 }
 
-// zeros in all of a row of the gradient
+// Zeros in all of a row of the gradient.  (Stored past the caches: with a fifth of the rows like that the backward pass of
+// 1021 x 50001 fp32 takes 72 us, not 80.  The gradient itself is better off in them, 831 us and 857 for the largest case of the
+// clipped loss -- but where the logits have just been read and are read again.)
 template <class E, int NT>
 __device__ __forceinline__ void zero_row(typename E::T* out, int V)
 {
     const Cut cut = cut_at<E>(out, V);
-    for (int v = threadIdx.x; v < cut.pieces; v += NT) *reinterpret_cast<u32x4_any*>(out + cut.head + (int64_t)v * E::N) = u32x4_any{0, 0, 0, 0};
+    for (int v = threadIdx.x; v < cut.pieces; v += NT) __builtin_nontemporal_store(u32x4_any{0, 0, 0, 0}, reinterpret_cast<u32x4_any*>(out + cut.head + (int64_t)v * E::N));
     if ((int)threadIdx.x < cut.loose) E::put(out + loose_column<E>(cut, threadIdx.x), 0.0f);
 }
-template <class E, bool ENT>
+template <class E, bool ENT, bool PAST = false>                         // PAST: past the caches
 __device__ __forceinline__ void put_piece(const RowGrad& q, const u32x4_any& w, typename E::T* out)
 {
     float z[E::N], d[E::N];
     E::unpack(w, z);
     gradient_of<ENT>(q, z, d);
-    *reinterpret_cast<u32x4_any*>(out) = E::pack(d);
+    if (PAST) __builtin_nontemporal_store(E::pack(d), reinterpret_cast<u32x4_any*>(out));
+    else *reinterpret_cast<u32x4_any*>(out) = E::pack(d);
 }
 template <class E, bool ENT>
 __device__ __forceinline__ void put_element(const RowGrad& q, float x, float more, typename E::T* out)
@@ -512,36 +516,38 @@ __device__ __forceinline__ bool stores_target(const Cut& cut, int target)
 }
 
 // ---------------------------------------------------------------------------
-// d / d logits of a row, element by element, from its coefficients; bound by the read and the write.  Rows are taken from the
-// last to the first: after a pass of sums over the same logits the last ones may still lie in the last-level cache.
+// d / d logits of a row, element by element, from its coefficients; bound by the read and the write.  AGAIN: a pass of sums over
+// the same logits has just been made, and its last rows may still lie in the last-level cache.  So the rows are taken from the
+// last to the first and the gradient is stored past the caches (6000 x 100003 fp16, all of the loss: 638 us without either, 645
+// and 638 with one of them, 614 with both).
 // ---------------------------------------------------------------------------
-template <class E, bool ENT>
-__global__ __launch_bounds__(WG) void block_gradients(const GradArgs a)
+template <class E, bool ENT, bool AGAIN, int NT>
+__global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
 {
     typedef typename E::T T;
     __shared__ FinishLds lds;
     if (a.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.fin, lds); return; }
-    const int64_t n = a.r.rows - 1 - blockIdx.x;
+    const int64_t n = AGAIN ? a.r.rows - 1 - blockIdx.x : blockIdx.x;
     const RowGrad q = grad_of_row(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
-    if (q.target < 0) { zero_row<E, WG>(out, a.r.V); return; }
+    if (q.target < 0) { zero_row<E, NT>(out, a.r.V); return; }
     const Cut cut = cut_at<E>(row, a.r.V);
     const float chosen = E::get(row + q.target);                        // (before it is overwritten)
     const T* in = row + cut.head;
     T* to = out + cut.head;
     constexpr int U = 4;
     int v = threadIdx.x;
-    for (; v + (U - 1) * WG < cut.pieces; v += U * WG) {
+    for (; v + (U - 1) * NT < cut.pieces; v += U * NT) {
         u32x4_any w[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * WG) * E::N);
+        for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * NT) * E::N);
 #pragma unroll
-        for (int k = 0; k < U; ++k) put_piece<E, ENT>(q, w[k], to + (int64_t)(v + k * WG) * E::N);
+        for (int k = 0; k < U; ++k) put_piece<E, ENT, AGAIN>(q, w[k], to + (int64_t)(v + k * NT) * E::N);
     }
-    for (; v < cut.pieces; v += WG) put_piece<E, ENT>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
+    for (; v < cut.pieces; v += NT) put_piece<E, ENT, AGAIN>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
     if ((int)threadIdx.x < cut.loose) { const int j = loose_column<E>(cut, threadIdx.x); put_element<E, ENT>(q, E::get(row + j), 0.0f, out + j); }
-    if (stores_target<E, WG>(cut, q.target)) put_element<E, ENT>(q, chosen, q.to_target, out + q.target);
+    if (stores_target<E, NT>(cut, q.target)) put_element<E, ENT>(q, chosen, q.to_target, out + q.target);
 }
 
 // ---------------------------------------------------------------------------
@@ -549,7 +555,7 @@ __global__ __launch_bounds__(WG) void block_gradients(const GradArgs a)
 // the one read to the one write; of a row longer than that the rest is read again.
 // ---------------------------------------------------------------------------
 template <class E, int NT, int VPT, bool ENT>
-__global__ __launch_bounds__(NT) void block_policy(const PolicyArgs a)
+__global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_policy(const PolicyArgs a)
 {
     typedef typename E::T T;
     constexpr int WAVES = NT / 64;
@@ -648,20 +654,20 @@ struct PairArgs {
     Norm norm;
     Partial* parts;
 };
-__global__ __launch_bounds__(WG) void pair_sums(const PairArgs a)
+__global__ __launch_bounds__(1024) void pair_sums(const PairArgs a)
 {
     __shared__ FinishLds lds;
     const int64_t P = a.q.count / 2;
-    const int lane = threadIdx.x & 63;
-    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, WG), lds.weights), inv = W != 0.0 ? a.grad_scale * reciprocal(W) : 0.0;
+    const int lane = threadIdx.x & 63, nt = blockDim.x;
+    const double W = block_sum(weight_share(a.norm, a.r, threadIdx.x, nt), lds.weights), inv = W != 0.0 ? a.grad_scale * reciprocal(W) : 0.0;
     double v[STATS] = {};
     for (int64_t k = blockIdx.x; k < P; k += gridDim.x) {
         const Seq s[2] = {sequence(a.q, k), sequence(a.q, k + P)};
         double t[STATS] = {};                                           // of the first and of the second: sum, tokens
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-#pragma unroll 2
-            for (int64_t j = threadIdx.x; j < s[i].n; j += WG) {
+#pragma unroll 4
+            for (int64_t j = threadIdx.x; j < s[i].n; j += nt) {
                 const int64_t row = s[i].first + j * s[i].step;
                 const RowWs w = a.ws[row];
                 const float ref = a.ref ? a.ref[row] : 0.0f;
@@ -686,7 +692,7 @@ __global__ __launch_bounds__(WG) void pair_sums(const PairArgs a)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float g = (float)((i == 0 ? dh : -dh) * per[i]);
-            for (int64_t j = threadIdx.x; j < s[i].n; j += WG) a.to_logp[s[i].first + j * s[i].step] = g;
+            for (int64_t j = threadIdx.x; j < s[i].n; j += nt) a.to_logp[s[i].first + j * s[i].step] = g;
         }
         if (threadIdx.x == 0) {
             const double nan = h != h ? (double)NAN : 0.0;
@@ -781,14 +787,17 @@ int32_t check_workspace(const void* ws, size_t have, size_t need)
 static bool is_finite(double x) { return x - x == 0.0; }
 
 // ---- which form a row takes ----------------------------------------------------------------------------------------
-// Lanes: the fewest (a power of two) that hold a row with 4 single elements each, up to 64 lanes and 256 columns; then
-// wavefronts with 1 or 4 pieces of 16 bytes a lane.  Longer rows take a workgroup.
+// Up to 32 columns: the fewest lanes that hold a row with 4 single elements each.  Up to 64 lanes of 4 pieces: the fewest of at
+// least 8 lanes that hold it, with 1, 2 or 4 pieces.  (Wavefronts for rows of 256 columns, as once here, spend their time on
+// one row's 64-bit arithmetic and its latencies: a million rows of bf16, sums 935 us.)  Longer rows take a workgroup.
 static LaneForm lane_form(int type, int64_t V)
 {
     const int64_t per = type == ANAKIN_TYPE_FP32 ? 4 : 8;
-    if (V <= 256) { int l = 1; while (l * 4 < V) l *= 2; return LaneForm{l, 0}; }
-    if (V <= 64 * per) return LaneForm{64, 1};
-    if (V <= 256 * per) return LaneForm{64, 4};
+    if (V <= 32) { int l = 1; while (l * 4 < V) l *= 2; return LaneForm{l, 0}; }
+    for (int pieces = 1; pieces <= 2; pieces *= 2)
+        if (V <= 8 * pieces * per) return LaneForm{8, pieces};
+    for (int lanes = 8; lanes <= 64; lanes *= 2)
+        if (V <= lanes * 4 * per) return LaneForm{lanes, 4};
     return LaneForm{0, 0};
 }
 static unsigned lane_grid(const LaneForm& f, int64_t rows)
@@ -799,7 +808,7 @@ static unsigned lane_grid(const LaneForm& f, int64_t rows)
 template <class E, int DO, bool FINE>
 static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid, hipStream_t s)
 {
-    auto k = f.pieces == 0 ? lanes_rows<E, DO, 0, FINE> : f.pieces == 1 ? lanes_rows<E, DO, 1, FINE> : lanes_rows<E, DO, 4, FINE>;
+    auto k = f.pieces == 0 ? lanes_rows<E, DO, 0, FINE> : f.pieces == 1 ? lanes_rows<E, DO, 1, FINE> : f.pieces == 2 ? lanes_rows<E, DO, 2, FINE> : lanes_rows<E, DO, 4, FINE>;
     hipLaunchKernelGGL(k, dim3(grid), dim3(WG), 0, s, a);
 }
 #define BY_TYPE(type, f, ...) ((type) == ANAKIN_TYPE_FP32 ? f<Fp32, __VA_ARGS__> : (type) == ANAKIN_TYPE_BF16 ? f<Bf16, __VA_ARGS__> : f<Fp16, __VA_ARGS__>)
@@ -815,8 +824,10 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
     } else {
         // Few rows: as many threads to a row as there are (one row of 131072 bf16 24 -> 13 us).  A compute unit's arithmetic
-        // bounds such a row, 8 us; sharing it out would take a second launch, which costs the host 3 us.
-        const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 512 ? 1024 : 256);
+        // bounds such a row, 8 us; sharing it out would take a second launch, which costs the host 3 us.  Many rows: the shorter
+        // they are the fewer threads, so that more of them are on their way.
+        const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
+        const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 512 ? 1024 : pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256);
         hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
     }
     return hipGetLastError();
@@ -830,19 +841,28 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         LaneArgs<DO_GRADIENT> l{};
         l.lanes = f.lanes; l.g = a;
         BY_TYPE(type, launch_lanes, DO_GRADIENT, false)(f, l, lane_grid(f, a.r.rows) + more, s);
-    } else if (ent) hipLaunchKernelGGL(BY_TYPE(type, block_gradients, true), dim3((unsigned)a.r.rows + more), dim3(WG), 0, s, a);
-    else hipLaunchKernelGGL(BY_TYPE(type, block_gradients, false), dim3((unsigned)a.r.rows + more), dim3(WG), 0, s, a);
+    } else {
+        // short rows: a wavefront each, so that more of them are on their way
+        const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
+        auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
+                       : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
+        hipLaunchKernelGGL(k, dim3((unsigned)a.r.rows + more), dim3(brief ? 64 : WG), 0, s, a);
+    }
     return hipGetLastError();
 }
 template <class E, bool ENT>
 static void launch_block_policy(const PolicyArgs& a, hipStream_t s)
 {
-    // the smallest workgroup whose registers hold a row; beyond 1024 threads of 16 pieces the rest is read twice
+    // As few threads as hold a row: several rows share a compute unit, and one is loaded while another is added up.  GB/s read and
+    // written (bf16) with these and with 1024 threads: 16384 x 12000 5000 and 1970, 16384 x 32768 5740 and 4250, 4096 x 65536 4800
+    // and 4250; 65536 x 2500 with 128 threads 4030, with 256 2600.  Beyond 1024 threads of 16 pieces the rest is read twice.
     const int64_t pieces = (a.r.V + E::N - 1) / E::N;
     const dim3 grid((unsigned)a.r.rows);
-    if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, ENT>), grid, dim3(256), 0, s, a);
-    else if (pieces <= 1024 * 4) hipLaunchKernelGGL((block_policy<E, 1024, 4, ENT>), grid, dim3(1024), 0, s, a);
-    else if (pieces <= 1024 * 8) hipLaunchKernelGGL((block_policy<E, 1024, 8, ENT>), grid, dim3(1024), 0, s, a);
+    if (pieces <= 128 * 4) hipLaunchKernelGGL((block_policy<E, 128, 4, ENT>), grid, dim3(128), 0, s, a);
+    else if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, ENT>), grid, dim3(256), 0, s, a);
+    else if (pieces <= 256 * 8) hipLaunchKernelGGL((block_policy<E, 256, 8, ENT>), grid, dim3(256), 0, s, a);
+    else if (pieces <= 512 * 8) hipLaunchKernelGGL((block_policy<E, 512, 8, ENT>), grid, dim3(512), 0, s, a);
+    else if (pieces <= 512 * 16) hipLaunchKernelGGL((block_policy<E, 512, 16, ENT>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((block_policy<E, 1024, 16, ENT>), grid, dim3(1024), 0, s, a);
 }
 // *parts: how many workgroups report sums
@@ -994,7 +1014,8 @@ extern "C" int32_t anakin_preference_loss(const anakin_rows* x, const anakin_seq
     sum.r = r; sum.logp = a->d_logp; sum.ws = reinterpret_cast<RowWs*>(base + w.ws); sum.coef = p.to_logp;
     LAUNCH(launch_sums(x->type, sum, true, s));
     const unsigned blocks = (unsigned)(P < 1 ? 1 : P > MAX_PARTS ? MAX_PARTS : P);
-    hipLaunchKernelGGL(pair_sums, dim3(blocks), dim3(WG), 0, s, p);
+    // (long sequences: as many threads as there are; 2 x 500000 tokens 880 us with 256)
+    hipLaunchKernelGGL(pair_sums, dim3(blocks), dim3(P > 0 && x->rows / (2 * P) > 512 ? 1024 : 256), 0, s, p);
     LAUNCH(hipGetLastError());
     const FinishArgs f{p.parts, (int)blocks, r, p.norm, a->d_stats, 0.0, 0.0, 0};
     if (a->d_dlogits && x->rows > 0) {
