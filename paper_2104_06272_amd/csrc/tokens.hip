@@ -268,75 +268,113 @@ template <> struct LaneArgs<DO_SUMS> { SumArgs s; int lanes; __device__ const Ro
 template <> struct LaneArgs<DO_GRADIENT> { GradArgs g; int lanes; __device__ const Rows& rows() const { return g.r; } };
 template <> struct LaneArgs<DO_POLICY> { PolicyArgs p; int lanes; __device__ const Rows& rows() const { return p.r; } };
 
+// what a lane holds of a row: `slots` of its P groups of W elements are in use (the same in all of a wavefront, which passes over
+// the others), and VECTOR a loose element
 template <class E, int PIECES>
 struct LaneRow {
     typedef typename E::T T;
     static constexpr bool VECTOR = PIECES > 0;
-    static constexpr int NE = VECTOR ? PIECES * E::N + 1 : 4;           // VECTOR: the last one is loose
-    static __device__ __forceinline__ void load(const T* row, const Cut& cut, int V, int lanes, int l, float (&z)[NE])
+    static constexpr int P = VECTOR ? PIECES : 1, W = VECTOR ? E::N : 4;
+    float z[P][W], loose[1];
+
+    static __device__ __forceinline__ int slots(int V, int lanes) { return VECTOR ? (V / W + lanes - 1) / lanes : 1; }
+    __device__ __forceinline__ void load(const T* row, const Cut& cut, int V, int lanes, int l, int slots)
     {
-        if constexpr (VECTOR) {
+        loose[0] = -INFINITY;
+        if constexpr (VECTOR && W == 8) {
+            // all loads before the first use: a million rows of 256 bf16, sums 169 -> 140 us (fp32 as below: 116, so 168)
+            u32x4_any w[P];
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k) {
-                const int v = k * lanes + l;
-                float f[E::N];
-                if (v < cut.pieces) E::unpack(*reinterpret_cast<const u32x4_any*>(row + cut.head + v * E::N), f);
+            for (int k = 0; k < P; ++k) if (k * lanes + l < cut.pieces) w[k] = *reinterpret_cast<const u32x4_any*>(row + cut.head + (k * lanes + l) * W);
 #pragma unroll
-                for (int i = 0; i < E::N; ++i) z[k * E::N + i] = v < cut.pieces ? f[i] : -INFINITY;
+            for (int k = 0; k < P; ++k) {
+                if (k >= slots) continue;
+                E::unpack(w[k], z[k]);
+                if (k == slots - 1 && k * lanes + l >= cut.pieces)
+#pragma unroll
+                    for (int i = 0; i < W; ++i) z[k][i] = -INFINITY;
             }
-            z[NE - 1] = l < cut.loose ? E::get(row + loose_column<E>(cut, l)) : -INFINITY;
-        } else {
+        } else if constexpr (VECTOR) {
 #pragma unroll
-            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; z[k] = j < V ? E::get(row + j) : -INFINITY; }
-        }
-    }
-    // the gradient d, and `more` at column `target`
-    static __device__ __forceinline__ void store(T* out, const Cut& cut, int V, int lanes, int l, float (&d)[NE], int target, float more)
-    {
-        if constexpr (VECTOR) {
-            const int tv = target >= cut.head ? (target - cut.head) / E::N : -1, ti = (target - cut.head) % E::N;
-#pragma unroll
-            for (int k = 0; k < PIECES; ++k) {
+            for (int k = 0; k < P; ++k) {
                 const int v = k * lanes + l;
-                if (v < cut.pieces) {
-                    float f[E::N];
+                if (k < slots && v < cut.pieces) E::unpack(*reinterpret_cast<const u32x4_any*>(row + cut.head + v * W), z[k]);
+                else {
 #pragma unroll
-                    for (int i = 0; i < E::N; ++i) f[i] = d[k * E::N + i] + (v == tv && i == ti ? more : 0.0f);
-                    *reinterpret_cast<u32x4_any*>(out + cut.head + v * E::N) = E::pack(f);
+                    for (int i = 0; i < W; ++i) z[k][i] = -INFINITY;
                 }
             }
-            if (l < cut.loose) { const int j = loose_column<E>(cut, l); E::put(out + j, d[NE - 1] + (j == target ? more : 0.0f)); }
+        }
+        if constexpr (VECTOR) {
+            if (l < cut.loose) loose[0] = E::get(row + loose_column<E>(cut, l));
         } else {
 #pragma unroll
-            for (int k = 0; k < NE; ++k) { const int j = k * lanes + l; if (j < V) E::put(out + j, d[k] + (j == target ? more : 0.0f)); }
+            for (int k = 0; k < W; ++k) { const int j = k * lanes + l; z[0][k] = j < V ? E::get(row + j) : -INFINITY; }
+        }
+    }
+    template <bool FINE>
+    __device__ __forceinline__ Sums sums(const Rows& r, int lanes, int slots) const
+    {
+        float m = loose[0];
+#pragma unroll
+        for (int k = 0; k < P; ++k) if (k < slots) m = max_of(z[k], m);
+        for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+        Part p{m, 0.0f, 0.0f};
+        const Shift s = shift_of(m, r.c);
+        const float m0 = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int k = 0; k < P; ++k) if (k < slots) add_at<FINE>(p, z[k], m0, s, r.c, r.c_lo);
+        if constexpr (VECTOR) add_at<FINE>(p, loose, m0, s, r.c, r.c_lo);
+        if (FINE) {
+            double d = fma(LN2, (double)p.u, (double)p.s);
+            for (int off = 1; off < lanes; off <<= 1) d += __shfl_xor(d, off, 64);
+            return Sums{m, d, 0.0};
+        }
+        for (int off = 1; off < lanes; off <<= 1) { p.s += __shfl_xor(p.s, off, 64); p.u += __shfl_xor(p.u, off, 64); }
+        return Sums{m, (double)p.s, (double)p.u};
+    }
+    // the row's gradient to `out` (of a row without a target z is all zeros, as are the coefficients)
+    template <bool ALL>                                                 // all of it before the first store (more registers)
+    __device__ __forceinline__ void put_gradient(const RowGrad& q, T* out, const Cut& cut, int V, int lanes, int l, int slots) const
+    {
+        if constexpr (VECTOR) {
+            const int tp = q.target - cut.head, tv = tp >= 0 ? tp / W : -1, ti = tp % W;
+            float d[ALL ? P : 1][W];
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                if (k >= slots) continue;
+                float (&dk)[W] = d[ALL ? k : 0];
+                const int v = k * lanes + l;
+                gradient_of<true>(q, z[k], dk);
+#pragma unroll
+                for (int i = 0; i < W; ++i) dk[i] += (ALL ? v * W + i == tp : v == tv && i == ti) ? q.to_target : 0.0f;
+                if (!ALL && v < cut.pieces) *reinterpret_cast<u32x4_any*>(out + cut.head + v * W) = E::pack(dk);
+            }
+            if (ALL)
+#pragma unroll
+                for (int k = 0; k < P; ++k) if (k * lanes + l < cut.pieces) *reinterpret_cast<u32x4_any*>(out + cut.head + (k * lanes + l) * W) = E::pack(d[k]);
+            if (l < cut.loose) {
+                const int j = loose_column<E>(cut, l);
+                float d[1];
+                gradient_of<true>(q, loose, d);
+                E::put(out + j, d[0] + (j == q.target ? q.to_target : 0.0f));
+            }
+        } else {
+            float d[W];
+            gradient_of<true>(q, z[0], d);
+#pragma unroll
+            for (int k = 0; k < W; ++k) { const int j = k * lanes + l; if (j < V) E::put(out + j, d[k] + (j == q.target ? q.to_target : 0.0f)); }
         }
     }
 };
-template <bool FINE, int NE>
-__device__ __forceinline__ Sums lanes_part(const float (&z)[NE], const Rows& r, int lanes)
-{
-    float m = max_of(z, -INFINITY);
-    for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    Part p{m, 0.0f, 0.0f};
-    add_at<FINE>(p, z, m == -INFINITY ? 0.0f : m, shift_of(m, r.c), r.c, r.c_lo);
-    if (FINE) {
-        double d = fma(LN2, (double)p.u, (double)p.s);
-        for (int off = 1; off < lanes; off <<= 1) d += __shfl_xor(d, off, 64);
-        return Sums{m, d, 0.0};
-    }
-    for (int off = 1; off < lanes; off <<= 1) { p.s += __shfl_xor(p.s, off, 64); p.u += __shfl_xor(p.u, off, 64); }
-    return Sums{m, (double)p.s, (double)p.u};
-}
 
 template <class E, int DO, int PIECES, bool FINE>
-__global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
+__global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_rows(const LaneArgs<DO> a)
 {
     typedef typename E::T T;
-    typedef LaneRow<E, PIECES> L;
-    constexpr int NE = L::NE;
     __shared__ FinishLds lds;
     const Rows& r = a.rows();
-    const int lanes = a.lanes, l = threadIdx.x & (lanes - 1), per = WG / lanes, V = r.V;
+    const int lanes = a.lanes, l = threadIdx.x & (lanes - 1), per = WG / lanes, V = r.V, slots = LaneRow<E, PIECES>::slots(V, lanes);
     int64_t grid = gridDim.x;
     if constexpr (DO == DO_GRADIENT) {
         if (a.g.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.g.fin, lds); return; }
@@ -351,56 +389,39 @@ __global__ __launch_bounds__(WG) void lanes_rows(const LaneArgs<DO> a)
         const int64_t n = base + threadIdx.x / lanes;
         const bool there = n < r.rows;
         const T* row = static_cast<const T*>(r.logits) + (there ? n : 0) * r.stride;
-        int target = -1;
-        float z[NE], d[NE];
+        const Cut cut = cut_at<E>(row, V, lanes >= 16);
+        LaneRow<E, PIECES> x{};
         if constexpr (DO == DO_GRADIENT) {
             if (!there) continue;
             const RowGrad q = grad_of_row(a.g, n);
-            target = q.target;
-            T* out = static_cast<T*>(a.g.out) + n * a.g.out_stride;
-            const Cut cut = cut_at<E>(row, V, lanes >= 16);
-            if (target >= 0) { L::load(row, cut, V, lanes, l, z); gradient_of<true>(q, z, d); }
-            else {
-#pragma unroll
-                for (int k = 0; k < NE; ++k) d[k] = 0.0f;
+            if (q.target >= 0) x.load(row, cut, V, lanes, l, slots);
+            x.template put_gradient<E::N == 8>(q, static_cast<T*>(a.g.out) + n * a.g.out_stride, cut, V, lanes, l, slots);
+        } else {
+            int target = -1;
+            PolicyIn in{};
+            if constexpr (DO == DO_POLICY) {
+                if (there) target = policy_target(a.p, n);
+                if (target >= 0) in = policy_in(a.p.p, n);
+            } else if (there) target = row_target(r, n);
+            if (target >= 0) x.load(row, cut, V, lanes, l, slots);
+            const float chosen = target >= 0 ? E::get(row + target) : 0.0f;
+            const Sums p = x.template sums<FINE>(r, lanes, slots);
+            if constexpr (DO == DO_SUMS) {
+                if (there && l == 0) store_sums<FINE>(a.s, n, p, target, chosen);
+            } else {
+                RowGrad q{};
+                double lp = 0.0;
+                q.target = -1;
+                if (target >= 0) {
+                    const RowSum y = finish_row<false>(p, r);
+                    lp = logp_of<false>(y, chosen, r);
+                    const PolicyRow z = policy_row(a.p.p, in, lp, y.entropy, y.empty);
+                    if (l == 0) add_stats(v, z);
+                    q = row_gradient(y, z.g * inv, z.e * inv, target, r.scale);
+                }
+                if (there && l == 0 && a.p.logp) a.p.logp[n] = (float)lp;
+                if (there && a.p.out) x.template put_gradient<false>(q, static_cast<T*>(a.p.out) + n * a.p.out_stride, cut, V, lanes, l, slots);
             }
-            L::store(out, cut, V, lanes, l, d, target, q.to_target);
-        } else {
-        PolicyIn in{};
-        if constexpr (DO == DO_POLICY) {
-            if (there) target = policy_target(a.p, n);
-            if (target >= 0) in = policy_in(a.p.p, n);
-        } else if (there) target = row_target(r, n);
-        const Cut cut = cut_at<E>(row, V, lanes >= 16);
-        if (target >= 0) L::load(row, cut, V, lanes, l, z);
-        else {
-#pragma unroll
-            for (int k = 0; k < NE; ++k) z[k] = 0.0f;
-        }
-        const Sums p = lanes_part<FINE>(z, r, lanes);
-        const float chosen = target >= 0 ? E::get(row + target) : 0.0f;
-        if constexpr (DO == DO_SUMS) {
-            if (there && l == 0) store_sums<FINE>(a.s, n, p, target, chosen);
-        } else {
-        RowGrad q{};
-        double lp = 0.0;
-        q.target = -1;
-        if (target >= 0) {
-            const RowSum x = finish_row<false>(p, r);
-            lp = logp_of<false>(x, chosen, r);
-            const PolicyRow y = policy_row(a.p.p, in, lp, x.entropy, x.empty);
-            if (l == 0) add_stats(v, y);
-            q = row_gradient(x, y.g * inv, y.e * inv, target, r.scale);
-        }
-        if (there && l == 0 && a.p.logp) a.p.logp[n] = (float)lp;
-        if (!there || !a.p.out) continue;
-        if (target >= 0) gradient_of<true>(q, z, d);
-        else {
-#pragma unroll
-            for (int k = 0; k < NE; ++k) d[k] = 0.0f;
-        }
-        L::store(static_cast<T*>(a.p.out) + n * a.p.out_stride, cut, V, lanes, l, d, target, q.to_target);
-        }
         }
     }
     if constexpr (DO == DO_POLICY) {
@@ -552,7 +573,8 @@ __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
 
 // ---------------------------------------------------------------------------
 // The clipped loss over long rows: a workgroup of NT threads holds a row in registers, VPT pieces of 16 bytes a thread, from
-// the one read to the one write; of a row longer than that the rest is read again.
+// the one read to the one write; of a row longer than that the rest is read again.  (Nine pieces more a thread in LDS gained 3 to
+// 5 % on fp32 rows of 100000 to 262144 columns and lost 1 % on bf16 ones of 200000: the second read comes from the caches.)
 // ---------------------------------------------------------------------------
 template <class E, int NT, int VPT, bool ENT>
 __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_policy(const PolicyArgs a)
@@ -720,7 +742,7 @@ int32_t fail_hip(hipError_t e)
 static int type_bytes(int type) { return type == ANAKIN_TYPE_FP32 ? 4 : 2; }
 
 struct LaneForm { int lanes; int pieces; };       // pieces 0: single elements; lanes 0: longer than that
-static LaneForm lane_form(int type, int64_t V);
+static LaneForm lane_form(int type, int64_t V, bool policy);
 constexpr int MAX_PARTS = 2048;                   // workgroups of short rows (8 for every compute unit) and of pairs that report sums at most
 
 // log-probabilities need none; the clipped loss room for the weights' and the workgroups' sums; pairs rows of their own too
@@ -731,7 +753,7 @@ static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
     w.weights = take(WEIGHT_PARTS * sizeof(double));
-    const bool lanes = lane_form(ANAKIN_TYPE_FP32, vocab).lanes > 0;    // (fp32 rows are the first to take workgroups)
+    const bool lanes = lane_form(ANAKIN_TYPE_FP32, vocab, true).lanes > 0 && lane_form(ANAKIN_TYPE_BF16, vocab, true).lanes > 0;
     w.parts = take((size_t)(!lanes && rows > MAX_PARTS ? rows : MAX_PARTS) * sizeof(Partial));
     w.folded = take(FOLDED * sizeof(Partial));
     w.ws = take(pairs ? (size_t)rows * sizeof(RowWs) : 0);
@@ -787,16 +809,19 @@ int32_t check_workspace(const void* ws, size_t have, size_t need)
 static bool is_finite(double x) { return x - x == 0.0; }
 
 // ---- which form a row takes ----------------------------------------------------------------------------------------
-// Up to 32 columns: the fewest lanes that hold a row with 4 single elements each.  Up to 64 lanes of 4 pieces: the fewest of at
+// Up to 32 columns: the fewest lanes that hold a row with 4 single elements each.  Up to 32 lanes of 4 pieces: the fewest of at
 // least 8 lanes that hold it, with 1, 2 or 4 pieces.  (Wavefronts for rows of 256 columns, as once here, spend their time on
-// one row's 64-bit arithmetic and its latencies: a million rows of bf16, sums 935 us.)  Longer rows take a workgroup.
-static LaneForm lane_form(int type, int64_t V)
+// one row's 64-bit arithmetic and its latencies: a million rows of bf16, sums 935 us against 173.)  Longer rows take a workgroup,
+// of 64 threads at first: 131072 x 2048 bf16, clipped loss 196 us against 376 with 64 lanes of 4 pieces here, 65536 x 1024 fp32
+// 200 and 250; the clipped loss over 16-bit rows does from 16 lanes of 4 pieces on (262144 x 1024 266 and 371; 524288 x 512 458
+// and 368), for which it has too many registers.
+static LaneForm lane_form(int type, int64_t V, bool policy)
 {
     const int64_t per = type == ANAKIN_TYPE_FP32 ? 4 : 8;
     if (V <= 32) { int l = 1; while (l * 4 < V) l *= 2; return LaneForm{l, 0}; }
     for (int pieces = 1; pieces <= 2; pieces *= 2)
         if (V <= 8 * pieces * per) return LaneForm{8, pieces};
-    for (int lanes = 8; lanes <= 64; lanes *= 2)
+    for (int lanes = 8; lanes <= (policy && per == 8 ? 16 : 32); lanes *= 2)
         if (V <= lanes * 4 * per) return LaneForm{lanes, 4};
     return LaneForm{0, 0};
 }
@@ -816,7 +841,7 @@ static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid
 static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t s)
 {
     if (a.r.rows == 0) return hipSuccess;
-    const LaneForm f = lane_form(type, a.r.V);
+    const LaneForm f = lane_form(type, a.r.V, false);
     if (f.lanes) {
         LaneArgs<DO_SUMS> l{};
         l.lanes = f.lanes; l.s = a;
@@ -835,7 +860,7 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
 static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStream_t s)
 {
     const unsigned more = a.fin.stats ? 1 : 0;
-    const LaneForm f = lane_form(type, a.r.V);
+    const LaneForm f = lane_form(type, a.r.V, false);
     if (a.r.rows == 0 && !more) return hipSuccess;
     if (f.lanes) {
         LaneArgs<DO_GRADIENT> l{};
@@ -858,7 +883,8 @@ static void launch_block_policy(const PolicyArgs& a, hipStream_t s)
     // and 4250; 65536 x 2500 with 128 threads 4030, with 256 2600.  Beyond 1024 threads of 16 pieces the rest is read twice.
     const int64_t pieces = (a.r.V + E::N - 1) / E::N;
     const dim3 grid((unsigned)a.r.rows);
-    if (pieces <= 128 * 4) hipLaunchKernelGGL((block_policy<E, 128, 4, ENT>), grid, dim3(128), 0, s, a);
+    if (pieces <= 64 * 4) hipLaunchKernelGGL((block_policy<E, 64, 4, ENT>), grid, dim3(64), 0, s, a);
+    else if (pieces <= 128 * 4) hipLaunchKernelGGL((block_policy<E, 128, 4, ENT>), grid, dim3(128), 0, s, a);
     else if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, ENT>), grid, dim3(256), 0, s, a);
     else if (pieces <= 256 * 8) hipLaunchKernelGGL((block_policy<E, 256, 8, ENT>), grid, dim3(256), 0, s, a);
     else if (pieces <= 512 * 8) hipLaunchKernelGGL((block_policy<E, 512, 8, ENT>), grid, dim3(512), 0, s, a);
@@ -870,7 +896,7 @@ static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipSt
 {
     *parts = 0;
     if (a.r.rows == 0) return hipSuccess;
-    const LaneForm f = lane_form(type, a.r.V);
+    const LaneForm f = lane_form(type, a.r.V, true);
     if (f.lanes) {
         LaneArgs<DO_POLICY> l{};
         l.lanes = f.lanes; l.p = a;
