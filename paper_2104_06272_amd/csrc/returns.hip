@@ -39,6 +39,7 @@ struct ReturnsArgs {
 
 // The map of everything behind this thread's piece in its column of the workgroup (threads piece * W + column), and of the
 // whole column from piece 0 on.  lds: [waves][W]
+template <bool WHOLE>
 __device__ __forceinline__ void block_maps(const Map& own, int W, Map* lds, Map& behind, Map& whole)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -56,6 +57,7 @@ __device__ __forceinline__ void block_maps(const Map& own, int W, Map* lds, Map&
     Map later{1.0, 0.0};
     for (int w = wave + 1; w < waves && later.a != 0.0; ++w) later = composed(later, lds[w * W + col]);
     behind = composed(next, later);
+    if (!WHOLE) return;
     whole = lds[col];
     for (int w = 1; w < waves && whole.a != 0.0; ++w) whole = composed(whole, lds[w * W + col]);
 }
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(WG) void returns_rows(const ReturnsArgs a)
         own = composed(own, m[k]);
     }
     Map behind, whole;
-    block_maps(own, 1, lds, behind, whole);
+    block_maps<!APPLY>(own, 1, lds, behind, whole);
     if (!APPLY) {
         if (threadIdx.x == 0) a.maps[blockIdx.x] = whole;
         return;
@@ -187,47 +189,58 @@ __global__ __launch_bounds__(WG) void returns_rows(const ReturnsArgs a)
     }
 }
 
+// what a thread reads of its piece of a column
+struct Steps { float r[STEPS], v[STEPS + 1]; uint8_t d[STEPS]; };
+template <class E>
+__device__ __forceinline__ void load_column(const ReturnsArgs& a, int64_t j0, int64_t n, int64_t col, Steps& x)
+{
+    const typename E::T* value = static_cast<const typename E::T*>(a.value);
+    const int64_t S = a.q.count;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+        const bool in = j0 + k < n;
+        const int64_t i = (j0 + k) * S + col;
+        x.r[k] = in ? a.reward[i] : 0.0f; x.v[k] = in ? E::get(value + i) : 0.0f; x.d[k] = in && a.done ? a.done[i] : 0;
+    }
+    x.v[STEPS] = j0 + STEPS < n ? E::get(value + (j0 + STEPS) * S + col) : 0.0f;
+}
+
 template <class E, bool APPLY>
 __global__ __launch_bounds__(COLS_WG) void returns_columns(const ReturnsArgs a)
 {
     __shared__ Map lds[(COLS_WG / 64) * COLS_MAX];
-    const int W = a.width, lane_col = threadIdx.x % W, piece = threadIdx.x / W, pieces = COLS_WG / W;
+    const int W = a.width, lane_col = threadIdx.x % W, piece = threadIdx.x / W, pieces = blockDim.x / W;
     const int64_t S = a.q.count, T = a.q.length, col = (int64_t)(blockIdx.x % a.groups) * W + lane_col, tile_steps = (int64_t)pieces * STEPS;
-    const int64_t my_tile = blockIdx.x / a.groups;
-    const typename E::T* value = static_cast<const typename E::T*>(a.value);
+    const int64_t my_tile = a.walk ? a.tiles - 1 : blockIdx.x / a.groups;
     const bool mine = col < S;
-    const int64_t n = mine ? sequence(a.q, col).n : 0;
+    const int64_t n = mine ? sequence(a.q, col).n : 0;                 // (0: nothing of a column that is not there is read)
     const double end = mine && a.bootstrap ? (double)a.bootstrap[col] : 0.0;
     Map later{1.0, 0.0};                                               // of the tiles behind
-    if (APPLY && !a.walk) {
+    Steps next;
+    load_column<E>(a, my_tile * tile_steps + (int64_t)piece * STEPS, n, col, next);
+    if (APPLY && !a.walk && a.tiles > 1) {
         // of the other workgroups' maps: every piece takes its share of the tiles behind this one
         const int64_t rest = a.tiles - 1 - my_tile, per = (rest + pieces - 1) / pieces, t0 = my_tile + 1 + piece * per;
         Map c{1.0, 0.0}, behind;
         for (int64_t t = t0; t < t0 + per && t < a.tiles && mine && c.a != 0.0; ++t) c = composed(c, a.maps[t * S + col]);
-        block_maps(c, W, lds, behind, later);
+        block_maps<true>(c, W, lds, behind, later);
     }
-    for (int64_t tile = a.walk ? a.tiles - 1 : my_tile; tile >= 0; --tile) {
+    for (int64_t tile = my_tile; tile >= 0; --tile) {
         const int64_t j0 = tile * tile_steps + (int64_t)piece * STEPS;
-        float r[STEPS], v[STEPS + 1];
-        uint8_t d[STEPS];
-#pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
-            const bool in = mine && j0 + k < n;
-            const int64_t i = (j0 + k) * S + col;
-            r[k] = in ? a.reward[i] : 0.0f; v[k] = in ? E::get(value + i) : 0.0f; d[k] = in && a.done ? a.done[i] : 0;
-        }
-        v[STEPS] = mine && j0 + STEPS < n ? E::get(value + (j0 + STEPS) * S + col) : 0.0f;
+        const Steps x = next;
         Map m[STEPS], own{1.0, 0.0};
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
             const bool in = j0 + k < n, last = j0 + k + 1 == n;
-            const double disc = d[k] ? 0.0 : a.gamma, vnext = last ? end : (double)v[k + 1];
+            const double disc = x.d[k] ? 0.0 : a.gamma, vnext = last ? end : (double)x.v[k + 1];
             m[k].a = in && !last ? disc * a.lambda : 0.0;
-            m[k].b = in ? ((double)r[k] - (double)v[k]) + (disc != 0.0 ? disc * vnext : 0.0) : 0.0;
+            m[k].b = in ? ((double)x.r[k] - (double)x.v[k]) + (disc != 0.0 ? disc * vnext : 0.0) : 0.0;
             own = composed(own, m[k]);
         }
+        if (a.walk && tile > 0) load_column<E>(a, j0 - tile_steps, n, col, next);      // on its way while this tile is scanned
         Map behind, whole;
-        block_maps(own, W, lds, behind, whole);
+        if (APPLY && !a.walk) block_maps<false>(own, W, lds, behind, whole);
+        else block_maps<true>(own, W, lds, behind, whole);
         if (!APPLY) {
             if (mine && piece == 0) a.maps[tile * S + col] = whole;
             return;
@@ -236,33 +249,42 @@ __global__ __launch_bounds__(COLS_WG) void returns_columns(const ReturnsArgs a)
 #pragma unroll
         for (int k = STEPS - 1; k >= 0; --k) {
             A = applied(m[k], A);
-            if (mine && j0 + k < T) { const int64_t i = (j0 + k) * S + col; a.adv[i] = (float)A; a.ret[i] = (float)(A + (double)v[k]); }
+            if (mine && j0 + k < T) { const int64_t i = (j0 + k) * S + col; a.adv[i] = (float)A; a.ret[i] = (float)(A + (double)x.v[k]); }
         }
         if (!a.walk) return;
         later = composed(whole, later);
     }
 }
 
-static int columns_width(int64_t count) { int w = 1; while (w < COLS_MAX && w < count) w *= 2; return w; }
-static int64_t columns_groups(int64_t count) { const int w = columns_width(count); return (count + w - 1) / w; }
-static int64_t columns_tiles(int64_t count, int64_t length) { const int64_t t = (int64_t)(COLS_WG / columns_width(count)) * STEPS; return (length + t - 1) / t; }
-// Columns that give half the compute units a workgroup each walk their tiles in one launch; fewer share the tiles out.
-static bool columns_walk(int64_t count) { return columns_groups(count) >= 128; }
+// Columns of a workgroup, and pieces of 8 steps: what the time axis takes, up to 32 of them where that is all of it, else 16
+// (two workgroups to a compute unit).
+struct ColumnForm { int width, pieces; int64_t groups, tiles; bool walk; };
+static ColumnForm column_form(int64_t count, int64_t length)
+{
+    ColumnForm f{1, 1, 0, 0, false};
+    while (f.width < COLS_MAX && f.width < count) f.width *= 2;
+    const int most = length <= 32 * STEPS ? 32 : 16;
+    while (f.pieces * f.width < 64 || (f.pieces < most && f.pieces * STEPS < length) || (f.width < COLS_MAX && f.pieces * f.width < 256)) f.pieces *= 2;
+    f.groups = (count + f.width - 1) / f.width;
+    f.tiles = (length + f.pieces * STEPS - 1) / (f.pieces * STEPS);
+    // columns that give every compute unit a workgroup walk their tiles in one launch; fewer share the tiles out in two
+    f.walk = f.tiles > 1 && f.groups >= 256;
+    return f;
+}
 
 template <class E>
 static hipError_t launch_returns_of(ReturnsArgs& a, hipStream_t s)
 {
     if (a.q.layout == ANAKIN_LAYOUT_TIME) {
-        a.width = columns_width(a.q.count); a.tiles = (int)columns_tiles(a.q.count, a.q.length);
-        a.walk = a.tiles == 1 || columns_walk(a.q.count);
-        a.groups = (unsigned)columns_groups(a.q.count);
-        const dim3 grid(a.groups * (a.walk ? 1u : (unsigned)a.tiles));
-        if (!a.walk) {
-            hipLaunchKernelGGL((returns_columns<E, false>), grid, dim3(COLS_WG), 0, s, a);
+        const ColumnForm f = column_form(a.q.count, a.q.length);
+        a.width = f.width; a.tiles = (int)f.tiles; a.walk = f.walk; a.groups = (unsigned)f.groups;
+        const dim3 grid(a.groups * (f.walk ? 1u : (unsigned)f.tiles)), block(f.width * f.pieces);
+        if (!f.walk && f.tiles > 1) {
+            hipLaunchKernelGGL((returns_columns<E, false>), grid, block, 0, s, a);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL((returns_columns<E, true>), grid, dim3(COLS_WG), 0, s, a);
+        hipLaunchKernelGGL((returns_columns<E, true>), grid, block, 0, s, a);
         return hipGetLastError();
     }
     a.tiles = (int)((a.q.rows + ROWS_TILE - 1) / ROWS_TILE);
@@ -291,7 +313,7 @@ extern "C" size_t anakin_returns_workspace_bytes(int64_t rows, int64_t count)
     // a map for every tile of rows, or for every tile of every column (time-major: rows / count steps)
     const size_t by_rows = (size_t)((rows + ROWS_TILE - 1) / ROWS_TILE);
     size_t by_columns = 0;
-    if (count > 0 && rows % count == 0 && !columns_walk(count)) by_columns = (size_t)(columns_tiles(count, rows / count) * count);
+    if (count > 0 && rows % count == 0) { const ColumnForm f = column_form(count, rows / count); by_columns = f.walk ? 0 : (size_t)(f.tiles * count); }
     return up256((by_rows > by_columns ? by_rows : by_columns) * sizeof(Map)) + 256;
 }
 
