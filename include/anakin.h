@@ -331,7 +331,7 @@ int32_t anakin_peak_probe(int32_t kind, int32_t workgroups, void* scratch, size_
  * unequal length.  No handle: the caller passes device pointers, a workspace where the call has one (256-byte
  * aligned, of the size the matching *_workspace_bytes returns) and a stream of the device that holds them, which has to be the current device;
  * everything is enqueued on that stream, nothing synchronises, and nothing is kept between calls.  Two calls that may
- * overlap in time need workspaces of their own.  Calls can be captured into a HIP graph.  Errors are found on the host
+ * overlap in time need workspaces of their own.  Outputs do not overlap inputs except where that is said.  Calls can be captured into a HIP graph.  Errors are found on the host
  * before anything is enqueued; anakin_last_error(NULL) has the message (per thread).  Results do not depend on
  * scheduling: no floating-point atomics. */
 enum { ANAKIN_TYPE_FP32 = 0, ANAKIN_TYPE_BF16 = 1, ANAKIN_TYPE_FP16 = 2 };
@@ -339,7 +339,7 @@ enum { ANAKIN_INDEX_U8 = 0, ANAKIN_INDEX_I32 = 1, ANAKIN_INDEX_I64 = 2 };
 
 /* A matrix of logits [rows][vocab] of `type`, `row_stride` elements from row to row (>= vocab; columns adjacent), and
  * the column each row chose.  The policy is softmax(scale * logits): scale is one over the sampling temperature.
- * rows < 2^31, vocab < 2^28.  A logit of minus infinity is a choice that is not allowed.
+ * rows < 2^31 (above 512 columns 2^22, with shorter rows up to 2^26), vocab < 2^28.  A logit of minus infinity is a choice that is not allowed.
  * A row whose target lies outside [0, vocab) takes no part: its logits are not read and may hold anything. */
 typedef struct {
     const void* d_logits;

@@ -173,6 +173,7 @@ __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
     if (a.ws) {
         const RowWs w = a.ws[n];
         x.k = w.k; x.inv_s = w.inv_s;
+        x.empty = w.inv_s == 0.0f;                                      // (all of it minus infinity)
         return row_gradient(x, a.to_logp[n], 0.0, w.target, a.r.scale);
     }
     const int target = row_target(a.r, n);
@@ -838,6 +839,9 @@ static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid
 }
 #define BY_TYPE(type, f, ...) ((type) == ANAKIN_TYPE_FP32 ? f<Fp32, __VA_ARGS__> : (type) == ANAKIN_TYPE_BF16 ? f<Bf16, __VA_ARGS__> : f<Fp16, __VA_ARGS__>)
 
+// a launch counts its threads in 32 bits
+static bool fits(int64_t rows, int threads) { return (uint64_t)(rows + 1) * threads < ((uint64_t)1 << 32); }
+
 static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t s)
 {
     if (a.r.rows == 0) return hipSuccess;
@@ -853,6 +857,7 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         // they are the fewer threads, so that more of them are on their way.
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
         const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 512 ? 1024 : pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256);
+        if (!fits(a.r.rows, (int)block.x)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
     }
     return hipGetLastError();
@@ -868,6 +873,7 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         BY_TYPE(type, launch_lanes, DO_GRADIENT, false)(f, l, lane_grid(f, a.r.rows) + more, s);
     } else {
         // short rows: a wavefront each, so that more of them are on their way
+        if (!fits(a.r.rows, WG)) return hipErrorInvalidConfiguration;
         const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
         auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
                        : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
@@ -905,6 +911,7 @@ static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipSt
         BY_TYPE(type, launch_lanes, DO_POLICY, false)(f, l, grid, s);
     } else {
         *parts = (int)a.r.rows;
+        if (!fits(a.r.rows, a.r.V > (type == ANAKIN_TYPE_FP32 ? 32768 : 65536) ? 1024 : 512)) return hipErrorInvalidConfiguration;
         if (a.p.ent != 0.0) BY_TYPE(type, launch_block_policy, true)(a, s);
         else BY_TYPE(type, launch_block_policy, false)(a, s);
     }

@@ -77,7 +77,9 @@ def ref_policy(x, old, adv, low, high, kl_coef, ref, ent, weight, norm):
     take = lambda v: float((w * torch.where(count, v, zero)).sum()) * inv
     policy, k, H = take(-torch.minimum(plain, clip)), take(kl), take(x["H"])
     stats = [policy + kl_coef * k - ent * H, policy, k, H, take((~inside).double()), take(r), W, float(on.sum())]
-    return stats, torch.where(count, g * w * inv, zero), torch.where(count, -ent * w * inv, zero), on
+    # g is a sum of two terms, each of which an error of lp changes by its own size (d(r A) = r A dlp, d(k e^d) = -k e^d dlp)
+    g_size = torch.where(inside, plain.abs(), 0.0) + kl_coef * (1 + torch.exp(d))
+    return stats, torch.where(count, g * w * inv, zero), torch.where(count, -ent * w * inv, zero), on, torch.where(count, g_size * w * inv, zero)
 
 
 def rows_of(layout, count, length, lengths):
@@ -149,7 +151,8 @@ def close_logp(r, x, V):
 def close_gradient(got, want, size, V, dtype):
     fi = torch.finfo(dtype)
     tiny = fi.smallest_normal * (1.0 if dtype == torch.float32 else fi.eps)           # flushed exponentials; subnormals' half steps
-    want, size = want.clamp(-fi.max, fi.max), size.nan_to_num(0, 0, 0)
+    size = size.nan_to_num(0, 0, 0)
+    want = torch.where(torch.isinf(want.to(dtype)), torch.sign(want) * math.inf, want)   # what the type cannot hold rounds to infinity
     close(got, want, fi.eps / 2 * want.abs().nan_to_num(0, 0, 0) + 4 * roundings(V) * size + tiny, "gradient")
 
 
@@ -170,7 +173,10 @@ def make_target(N, V, g, kind=torch.int64, skip=0.0, device="cuda"):
 
 SIZES = [(1, 1, 0), (3, 2, 0), (70, 3, 1), (5, 7, 0), (33, 8, 2), (9, 63, 1), (4, 64, 0), (130, 65, 0), (7, 255, 3), (3, 256, 0), (6, 1000, 0),
          (5, 1024, 0), (4, 1025, 7), (3, 2049, 0), (2, 4099, 1), (3, 8192, 8), (2, 16411, 0), (3, 32768, 0), (2, 50001, 3), (1, 65537, 0),
-         (2, 131072, 0), (1, 200003, 0), (1, 262145, 0)]
+         (2, 131072, 0), (1, 200003, 0), (1, 262145, 0),
+         # every form of short and long rows, and as many rows as take more than one workgroup's sums
+         (40, 100, 0), (40, 128, 2), (33, 300, 1), (20, 511, 0), (20, 513, 0), (9, 1023, 1), (5, 1500, 1), (4, 3000, 0), (3, 12000, 1), (2, 40000, 0), (2, 100003, 5),
+         (2500, 5, 0), (3000, 600, 1), (700, 2100, 1), (5000, 40, 3)]
 
 
 # ---- CPU: the statement itself, and refusals -------------------------------------------------------------------------
@@ -191,7 +197,7 @@ def test_reference_gradients_are_differences():
     def preference(z):
         return ref_preference(ref_rows(z, t, 0.7), rows, 0.6, 0.2, True, ref, label, pw, 0.0)
     x = ref_rows(z, t, 0.7)
-    _, g1, g2, _ = policy(z)
+    _, g1, g2, _, _ = policy(z)
     by_formula = ref_gradient(x, g1, g2, 0.7)[0], ref_gradient(x, preference(z)[2], torch.zeros(4).double(), 0.7)[0]
     step = 1e-5
     for f, want in zip((policy, preference), by_formula):
@@ -369,12 +375,13 @@ def test_policy_loss(dtype, N, V, pad):
         cu = lambda v: None if v is None else v.cuda()
         r = tokens.policy_loss(z, t, cu(old), cu(adv), clip=(0.2, 0.28), kl_coef=kl, logp_ref=cu(ref) if kl else None, entropy_coef=ent, weight=cu(w), norm=norm,
                                scale=scale, grad_scale=up)
-        stats, g1, g2, on = ref_policy(x, old, adv, 0.2, 0.28, kl, ref if kl else None, ent, w, norm)
+        stats, g1, g2, on, g_size = ref_policy(x, old, adv, 0.2, 0.28, kl, ref if kl else None, ent, w, norm)
         close(r.logp, torch.where(on, x["lp"], 0.0), U * x["lp"].abs() + 2 * roundings(V), "logp")
         size = 4.0 * (1 + torch.tensor(stats, dtype=torch.float64).abs() + float(adv.abs().max())) * (1.0 if not norm else max(1.0, float(weight.sum()) / norm))
         close(r.stats, torch.tensor(stats, dtype=torch.float64), size * roundings(V), "stats")
-        want, sz = ref_gradient(x, g1 * up, g2 * up, scale)
-        # the ratio carries the roundings of lp: an absolute error of lp is a relative one of g
+        want, _ = ref_gradient(x, g1 * up, g2 * up, scale)
+        # the ratio carries the roundings of lp: an absolute error of lp is a relative one of each term of g
+        _, sz = ref_gradient(x, g_size * up, g2 * up, scale)
         close_gradient(r.dlogits, want, 3 * sz, V, DT[dtype])
         alone = tokens.policy_loss(z, t, cu(old), cu(adv), clip=(0.2, 0.28), kl_coef=kl, logp_ref=cu(ref) if kl else None, entropy_coef=ent, weight=cu(w), norm=norm,
                                    scale=scale, gradient=False)
@@ -428,7 +435,7 @@ def test_masks_and_extremes(dtype, V):
     adv, w = torch.randn(N, generator=g), torch.rand(N, generator=g) + 0.1
     old = torch.where(torch.isfinite(x["lp"]), x["lp"] - 0.1, -2.0).float()
     p = tokens.policy_loss(zc, tc, old.cuda(), adv.cuda(), entropy_coef=0.01, weight=w.cuda(), grad_scale=64.0)
-    stats, g1, g2, on = ref_policy(x, old, adv, 0.2, 0.2, 0.0, None, 0.01, w, 0.0)
+    stats, g1, g2, on, _ = ref_policy(x, old, adv, 0.2, 0.2, 0.0, None, 0.01, w, 0.0)
     want, size = ref_gradient(x, 64 * g1, 64 * g2, 1.0)
     close(p.stats, torch.tensor(stats, dtype=torch.float64), 4 * (1 + torch.tensor(stats).double().abs() + 3) * roundings(V), "stats")
     close_gradient(p.dlogits, want, 3 * size, V, DT[dtype])
@@ -491,7 +498,7 @@ def _sequences(layout, count, g, longest, spare=0):
 @gpu
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("layout", ["packed", "batch", "time"])
-@pytest.mark.parametrize("pairs,longest,V", [(1, 1, 5), (3, 9, 33), (2, 300, 7), (5, 20, 1031), (2, 13, 40001), (40, 3, 300)])
+@pytest.mark.parametrize("pairs,longest,V", [(1, 1, 5), (3, 9, 33), (2, 300, 7), (5, 20, 1031), (2, 13, 40001), (40, 3, 300), (1, 1500, 5), (3000, 2, 4)])
 def test_preference_loss(dtype, layout, pairs, longest, V):
     g = torch.Generator().manual_seed(pairs * 31 + V)
     rows, N, seq = _sequences(layout, 2 * pairs, g, longest, spare=3)
@@ -515,7 +522,7 @@ def test_preference_loss(dtype, layout, pairs, longest, V):
         scale = max(1.0, (float(w.sum()) / norm) if norm else 1.0)
         close(r.stats[[0, 2, 3, 4, 5, 6, 7]], st[[0, 2, 3, 4, 5, 6, 7]], 2 * (per * scale + U * st[[0, 2, 3, 4, 5, 6, 7]].abs()), "stats")
         near = float((np.abs(h) <= per).sum())                    # pairs whose h the roundings may carry across 0
-        assert abs(float(r.stats[1]) - stats[1]) <= 2 * U + (near if near else 0.0)
+        assert abs(float(r.stats[1]) - stats[1]) <= 2 * U * max(1.0, abs(stats[1])) + (near if near else 0.0)      # (rounded to fp32: u of its size)
         want, size = ref_gradient(x, g1 * up, torch.zeros(N).double(), 0.9)
         close_gradient(r.dlogits, want, (1 + longest) * size, V, DT[dtype])
     assert torch.equal(room, before)
@@ -530,7 +537,7 @@ def test_preference_loss(dtype, layout, pairs, longest, V):
 @gpu
 @pytest.mark.parametrize("value", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("layout", ["packed", "batch", "time"])
-@pytest.mark.parametrize("count,longest", [(1, 1), (3, 5), (70, 3), (2, 700), (1, 5000), (300, 40), (5, 2049), (1, 70001), (64, 513), (1030, 17)])
+@pytest.mark.parametrize("count,longest", [(1, 1), (3, 5), (70, 3), (2, 700), (1, 5000), (300, 40), (5, 2049), (1, 70001), (64, 513), (1030, 17), (8300, 300), (20000, 5), (100, 2000), (5000, 2)])
 def test_lambda_returns(value, layout, count, longest):
     g = torch.Generator().manual_seed(count + longest)
     rows, N, seq = _sequences(layout, count, g, longest, spare=5)
@@ -571,6 +578,23 @@ def test_broken_sequences_stay_inside_the_rows():
         assert torch.isnan(tokens.preference_loss(z, t, seq).loss)
         adv, _ = tokens.lambda_returns(room[:N].contiguous(), room[:N].contiguous(), seq)
         assert torch.isfinite(adv).all()
+
+
+@gpu
+@pytest.mark.parametrize("V", [6, 300, 9000])
+def test_a_pair_with_an_impossible_token(V):
+    """A forbidden target, and a row that allows nothing: the log-probability of their sequence is minus infinity; the gradient stays
+    finite, and is zero where nothing is allowed."""
+    z, _, g = make_logits(8, V, "fp32")
+    t = make_target(8, V, g)
+    z[1, int(t[1])] = -math.inf
+    z[6] = -math.inf
+    r = tokens.preference_loss(z, t, tokens.batch_major(4, 2))
+    assert r.logp[1] == -math.inf and r.logp[6] == -math.inf
+    assert r.margins[0] == -math.inf and r.margins[1] == math.inf and r.loss == math.inf
+    assert torch.isfinite(r.dlogits).all() and not r.dlogits[6].any() and r.dlogits[0].any()
+    lost = tokens.policy_loss(z, t, torch.zeros(8, device="cuda"), torch.ones(8, device="cuda"), entropy_coef=0.1)
+    assert torch.isfinite(lost.stats).all() and torch.isfinite(lost.dlogits).all() and not lost.dlogits[6].any()
 
 
 @gpu
