@@ -166,6 +166,7 @@ struct GradArgs {
     const RowWs* ws;                             // of the first pass; null: from the caller's lse
     const float *lse, *entropy, *to_logp, *to_entropy;   // the caller's (to_entropy may be null); to_logp also with ws
     FinishArgs fin;                              // stats not null: a workgroup more finishes the statistics
+    int shares;                                  // long rows: workgroups to a row
 };
 __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
 {
@@ -549,27 +550,33 @@ __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
     typedef typename E::T T;
     __shared__ FinishLds lds;
     if (a.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.fin, lds); return; }
-    const int64_t n = AGAIN ? a.r.rows - 1 - blockIdx.x : blockIdx.x;
+    const int64_t n = AGAIN ? a.r.rows - 1 - blockIdx.x / a.shares : blockIdx.x / a.shares;
     const RowGrad q = grad_of_row(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
-    if (q.target < 0) { zero_row<E, NT>(out, a.r.V); return; }
+    constexpr int U = 4;
+    const int share = (int)(blockIdx.x % a.shares);                     // of the row, in whole rounds of U pieces a thread
+    if (q.target < 0) { if (share == 0) zero_row<E, NT>(out, a.r.V); return; }
     const Cut cut = cut_at<E>(row, a.r.V);
-    const float chosen = E::get(row + q.target);                        // (before it is overwritten)
+    const int rounds = (cut.pieces + U * NT - 1) / (U * NT), each = (rounds + a.shares - 1) / a.shares;
+    const int begin = share * each * U * NT, end = begin + each * U * NT < cut.pieces ? begin + each * U * NT : cut.pieces;
     const T* in = row + cut.head;
     T* to = out + cut.head;
-    constexpr int U = 4;
-    int v = threadIdx.x;
-    for (; v + (U - 1) * NT < cut.pieces; v += U * NT) {
+    // (the target's logit before it is overwritten; of a row in shares, by the one that stores it)
+    const int tp = q.target - cut.head, tv = tp >= 0 ? tp / E::N : 0;
+    const bool loose = tp < 0 || tv >= cut.pieces, mine = loose ? share == 0 : tv >= begin && tv < end;
+    const float chosen = mine ? E::get(row + q.target) : 0.0f;
+    int v = begin + threadIdx.x;
+    for (; v + (U - 1) * NT < end; v += U * NT) {
         u32x4_any w[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * NT) * E::N);
 #pragma unroll
         for (int k = 0; k < U; ++k) put_piece<E, ENT, AGAIN>(q, w[k], to + (int64_t)(v + k * NT) * E::N);
     }
-    for (; v < cut.pieces; v += NT) put_piece<E, ENT, AGAIN>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
-    if ((int)threadIdx.x < cut.loose) { const int j = loose_column<E>(cut, threadIdx.x); put_element<E, ENT>(q, E::get(row + j), 0.0f, out + j); }
-    if (stores_target<E, NT>(cut, q.target)) put_element<E, ENT>(q, chosen, q.to_target, out + q.target);
+    for (; v < end; v += NT) put_piece<E, ENT, AGAIN>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
+    if (share == 0 && (int)threadIdx.x < cut.loose) { const int j = loose_column<E>(cut, threadIdx.x); put_element<E, ENT>(q, E::get(row + j), 0.0f, out + j); }
+    if (mine && stores_target<E, NT>(cut, q.target)) put_element<E, ENT>(q, chosen, q.to_target, out + q.target);
 }
 
 // ---------------------------------------------------------------------------
@@ -852,11 +859,11 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         if (fine) BY_TYPE(type, launch_lanes, DO_SUMS, true)(f, l, lane_grid(f, a.r.rows), s);
         else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
     } else {
-        // Few rows: as many threads to a row as there are (one row of 131072 bf16 24 -> 13 us).  A compute unit's arithmetic
-        // bounds such a row, 8 us; sharing it out would take a second launch, which costs the host 3 us.  Many rows: the shorter
-        // they are the fewer threads, so that more of them are on their way.
+        // Fewer rows than compute units: 16 pieces a thread (one row of 131072 bf16 with 256 threads 15.4 us, with 1024 12.9; 64 x 8192
+        // 5.3 and 6.9).  Many rows: the shorter they are the fewer threads, so that more of them are on their way.
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
-        const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 512 ? 1024 : pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256);
+        const int few = pieces >= 12288 ? 1024 : pieces >= 6144 ? 512 : 256, many = pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256;
+        const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 256 ? few : a.r.rows <= 512 ? 256 : many);
         if (!fits(a.r.rows, (int)block.x)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
     }
@@ -877,7 +884,11 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
         auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
                        : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
-        hipLaunchKernelGGL(k, dim3((unsigned)a.r.rows + more), dim3(brief ? 64 : WG), 0, s, a);
+        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 4 us)
+        GradArgs b = a;
+        const int64_t rounds = a.r.V / ((type == ANAKIN_TYPE_FP32 ? 4 : 8) * 4 * WG);
+        b.shares = brief || a.r.rows >= 1024 || rounds < 2 ? 1 : (int)(1024 / (a.r.rows > 0 ? a.r.rows : 1) < rounds ? 1024 / (a.r.rows > 0 ? a.r.rows : 1) : rounds);
+        hipLaunchKernelGGL(k, dim3((unsigned)(a.r.rows * b.shares) + more), dim3(brief ? 64 : WG), 0, s, b);
     }
     return hipGetLastError();
 }
