@@ -2,12 +2,12 @@
 // the loss over pairs of sequences.  The mathematics of a row stands in tokens.h, that of the losses at policy_row and
 // pair_sums.  Three things are done with a row -- its sums, its gradient from given coefficients, and both with the clipped
 // loss between them -- and each comes in three forms by the length of a row:
-//   lanes_*    short rows: 1 to 64 lanes hold a row in registers, 64 / lanes rows to a wavefront
+//   lanes_rows short rows: 1 to 32 lanes hold a row in registers, 64 / lanes rows to a wavefront
 //   block_sums, block_gradients   a workgroup streams a row
 //   block_policy                  a workgroup holds a row in registers between its sums and its gradient
 // and   weight_sums   partial sums of the rows' (pairs') weights
 //       pair_sums     the pairs: summed log ratios, coefficients of their rows
-//       finish_stats  adds the workgroups' sums in a fixed order
+//       fold_stats, finish_stats  add the workgroups' sums in a fixed order
 #include <math.h>
 #include "tokens.h"
 
@@ -178,7 +178,7 @@ __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
         return row_gradient(x, a.to_logp[n], 0.0, w.target, a.r.scale);
     }
     const int target = row_target(a.r, n);
-    if (target < 0) return row_gradient(x, 0.0, 0.0, -1, 0.0);
+    if (target < 0) { RowGrad q{}; q.target = -1; return q; }
     // p_j = 2^(c z - K) / s with K = fl(lse log2 e) and the rest of lse in s.  (A log-sum-exp of 2^30 and more has no room for
     // probabilities: its neighbours are 64 apart.  The maximum's is 1 and nothing overflows.)
     const double e = a.to_entropy ? a.to_entropy[n] : 0.0, lse = a.lse[n], k = lse * LOG2E, zc = lse / a.r.scale;
@@ -259,7 +259,7 @@ __device__ __forceinline__ int policy_target(const PolicyArgs& a, int64_t n)
 }
 
 // ---------------------------------------------------------------------------
-// Short rows.  `lanes` lanes (a power of two up to 64) hold a row: PIECES of 16 bytes each, piece k lanes + l at lane l, and a
+// Short rows.  `lanes` lanes (a power of two up to 32) hold a row: PIECES of 16 bytes each, piece k lanes + l at lane l, and a
 // loose element (8 lanes: pieces from column 0 on, which leaves no more than 7 loose); or (PIECES 0) four single elements, element
 // k of lane l in column k lanes + l.  Everything of a row happens in registers; all its lanes carry out the row's 64-bit
 // arithmetic together, so that a row should have few of them.
@@ -770,6 +770,9 @@ static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
     return w;
 }
 
+// whether addresses of rows so far apart can be counted
+static bool spans(int64_t rows, int64_t stride) { return rows <= 1 || stride <= ((int64_t)1 << 50) / rows; }
+
 static int32_t check_rows(const anakin_rows* x, Rows& r)
 {
     if (!x) return fail(ANAKIN_E_INVALID_ARG, "null rows");
@@ -778,7 +781,7 @@ static int32_t check_rows(const anakin_rows* x, Rows& r)
     if (x->rows < 0 || x->rows > MAX_ROWS) return fail(ANAKIN_E_INVALID_ARG, "rows out of range");
     if (x->vocab < 1 || x->vocab > MAX_VOCAB) return fail(ANAKIN_E_INVALID_ARG, "vocab out of range");
     if (x->row_stride < x->vocab && x->rows > 1) return fail(ANAKIN_E_INVALID_ARG, "row_stride is less than vocab");
-    if (x->row_stride > ((int64_t)1 << 40)) return fail(ANAKIN_E_INVALID_ARG, "row_stride out of range");
+    if (!spans(x->rows, x->row_stride)) return fail(ANAKIN_E_INVALID_ARG, "row_stride out of range");
     if (!(x->scale >= 1e-6 && x->scale <= 1e6)) return fail(ANAKIN_E_INVALID_ARG, "scale has to lie in [1e-6, 1e6]");
     if (x->rows > 0 && (!x->d_logits || !x->d_target)) return fail(ANAKIN_E_INVALID_ARG, "null logits or targets");
     if ((uintptr_t)x->d_logits % type_bytes(x->type)) return fail(ANAKIN_E_MISALIGNED, "logits are not aligned to their type");
@@ -794,7 +797,7 @@ static int32_t check_gradient(const anakin_rows* x, const void* out, int64_t str
 {
     if (!out) return x->rows > 0 ? fail(ANAKIN_E_INVALID_ARG, "null gradient") : ANAKIN_OK;
     if (stride < x->vocab && x->rows > 1) return fail(ANAKIN_E_INVALID_ARG, "grad_stride is less than vocab");
-    if (stride > ((int64_t)1 << 40)) return fail(ANAKIN_E_INVALID_ARG, "grad_stride out of range");
+    if (!spans(x->rows, stride)) return fail(ANAKIN_E_INVALID_ARG, "grad_stride out of range");
     const int64_t b = type_bytes(x->type);
     if ((uintptr_t)out % b) return fail(ANAKIN_E_MISALIGNED, "gradient is not aligned to its type");
     if (x->rows == 0) return ANAKIN_OK;

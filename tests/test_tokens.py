@@ -233,7 +233,7 @@ def _policy(**over):
 
 
 BAD_ROWS = [dict(type=3), dict(type=-1), dict(target_type=3), dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=1 << 28), dict(row_stride=99), dict(scale=0.0),
-            dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-7), dict(logits=None), dict(target=None), dict(row_stride=1 << 41)]
+            dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-7), dict(logits=None), dict(target=None), dict(row_stride=1 << 50), dict(rows=(1 << 31) - 1, row_stride=1 << 31), dict(row_stride=-100)]
 
 
 @pytest.mark.parametrize("over", BAD_ROWS, ids=str)
@@ -578,6 +578,34 @@ def test_broken_sequences_stay_inside_the_rows():
         assert torch.isnan(tokens.preference_loss(z, t, seq).loss)
         adv, _ = tokens.lambda_returns(room[:N].contiguous(), room[:N].contiguous(), seq)
         assert torch.isfinite(adv).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [3, 70, 700, 5001, 70000])
+@pytest.mark.parametrize("begin,to", [(1, 1), (3, 0), (5, 2), (7, 7)])
+def test_rows_that_begin_anywhere(dtype, V, begin, to):
+    """Logits and gradients a few elements off their allocations' starts, alike and not: the formulas hold, and nothing around the
+    rows is written."""
+    N = 5
+    z, _, g = make_logits(N, V, dtype, seed=6)
+    buf, back = torch.full((N * V + 16,), 7.0, dtype=DT[dtype], device="cuda"), torch.full((N * V + 16,), 7.0, dtype=DT[dtype], device="cuda")
+    zb, out = buf[begin:begin + N * V].view(N, V), back[to:to + N * V].view(N, V)
+    zb.copy_(z)
+    before = buf.clone()
+    t = make_target(N, V, g)
+    t[2] = -1
+    x = ref_rows(zb, t, 1.0)
+    old, adv = (x["lp"] - 0.05).float(), torch.randn(N, generator=g)
+    p = tokens.policy_loss(zb, t, old.cuda(), adv.cuda(), entropy_coef=0.02, out=out)
+    _, g1, g2, on, size = ref_policy(x, old, adv, 0.2, 0.2, 0.0, None, 0.02, None, 0.0)
+    close_gradient(p.dlogits, ref_gradient(x, g1, g2, 1.0)[0], 3 * ref_gradient(x, size, g2, 1.0)[1], V, DT[dtype])
+    r = tokens.logprobs(zb, t)
+    close_logp(r, x, V)
+    d = tokens.logprobs_backward(zb, t, r.lse, adv.cuda(), out=out)
+    want, size = ref_gradient(x, adv.double(), torch.zeros(N).double(), 1.0)
+    close_gradient(d, want, size * (1 + x["lse"].abs()[:, None]), V, DT[dtype])
+    assert torch.equal(buf, before) and (back[:to] == 7).all() and (back[to + N * V:] == 7).all()
 
 
 @gpu
