@@ -339,7 +339,8 @@ enum { ANAKIN_INDEX_U8 = 0, ANAKIN_INDEX_I32 = 1, ANAKIN_INDEX_I64 = 2 };
 
 /* A matrix of logits [rows][vocab] of `type`, `row_stride` elements from row to row (>= vocab; columns adjacent), and
  * the column each row chose.  The policy is softmax(scale * logits): scale is one over the sampling temperature.
- * rows < 2^31 (above 512 columns 2^22, with shorter rows up to 2^26), vocab < 2^28.  A logit of minus infinity is a choice that is not allowed.
+ * vocab < 2^28; rows < 2^31, and above 512 columns as many as a launch can count: 2^26 - 2 up to 1024 fp32 or 2048 16-bit
+ * columns, 2^22 - 2 for the longest rows.  A logit of minus infinity is a choice that is not allowed.
  * A row whose target lies outside [0, vocab) takes no part: its logits are not read and may hold anything. */
 typedef struct {
     const void* d_logits;

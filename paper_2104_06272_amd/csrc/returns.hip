@@ -336,7 +336,7 @@ extern "C" int32_t anakin_lambda_returns(const anakin_sequences* q, const anakin
     if (a->rows == 0) return ANAKIN_OK;
     ReturnsArgs k{};
     k.q = Seqs{q->layout, q->count, q->length, a->rows, q->d_offsets, q->d_lengths};
-    if (q->layout == ANAKIN_LAYOUT_TIME && q->count == 1) k.q.layout = ANAKIN_LAYOUT_BATCH;      // one column is one run of rows
+    if (q->layout == ANAKIN_LAYOUT_TIME && (q->count == 1 || q->length == 1)) k.q.layout = ANAKIN_LAYOUT_BATCH;      // the same rows
     k.reward = a->d_reward; k.value = a->d_value; k.done = a->d_done; k.bootstrap = a->d_bootstrap; k.gamma = a->gamma; k.lambda = a->lambda_;
     k.adv = a->d_adv; k.ret = a->d_ret; k.maps = static_cast<Map*>(d_workspace);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -770,6 +770,16 @@ static RowsWs rows_workspace(int64_t rows, int64_t vocab, int64_t pairs)
     return w;
 }
 
+// A launch counts its threads in 32 bits.  Rows of more than 512 columns may take a workgroup each (and one that finishes): of
+// so many threads at most, where there are more than 512 of them.
+constexpr int64_t LANES_ALWAYS = 512;
+static int most_threads(int type, int64_t V)
+{
+    const int64_t per = type == ANAKIN_TYPE_FP32 ? 4 : 8, pieces = (V + per - 1) / per;
+    return pieces <= 256 ? 64 : pieces <= 512 ? 128 : pieces <= 2048 ? 256 : pieces <= 8192 ? 512 : 1024;
+}
+static bool fits(int64_t rows, int threads) { return (uint64_t)(rows + 1) * threads < ((uint64_t)1 << 32); }
+
 // whether addresses of rows so far apart can be counted
 static bool spans(int64_t rows, int64_t stride) { return rows <= 1 || stride <= ((int64_t)1 << 50) / rows; }
 
@@ -780,6 +790,7 @@ static int32_t check_rows(const anakin_rows* x, Rows& r)
     if (x->target_type < ANAKIN_INDEX_U8 || x->target_type > ANAKIN_INDEX_I64) return fail(ANAKIN_E_INVALID_ARG, "unknown type of the targets");
     if (x->rows < 0 || x->rows > MAX_ROWS) return fail(ANAKIN_E_INVALID_ARG, "rows out of range");
     if (x->vocab < 1 || x->vocab > MAX_VOCAB) return fail(ANAKIN_E_INVALID_ARG, "vocab out of range");
+    if (x->vocab > LANES_ALWAYS && !fits(x->rows, most_threads(x->type, x->vocab))) return fail(ANAKIN_E_INVALID_ARG, "more rows than a launch can count");
     if (x->row_stride < x->vocab && x->rows > 1) return fail(ANAKIN_E_INVALID_ARG, "row_stride is less than vocab");
     if (!spans(x->rows, x->row_stride)) return fail(ANAKIN_E_INVALID_ARG, "row_stride out of range");
     if (!(x->scale >= 1e-6 && x->scale <= 1e6)) return fail(ANAKIN_E_INVALID_ARG, "scale has to lie in [1e-6, 1e6]");
@@ -849,9 +860,6 @@ static void launch_lanes(const LaneForm& f, const LaneArgs<DO>& a, unsigned grid
 }
 #define BY_TYPE(type, f, ...) ((type) == ANAKIN_TYPE_FP32 ? f<Fp32, __VA_ARGS__> : (type) == ANAKIN_TYPE_BF16 ? f<Bf16, __VA_ARGS__> : f<Fp16, __VA_ARGS__>)
 
-// a launch counts its threads in 32 bits
-static bool fits(int64_t rows, int threads) { return (uint64_t)(rows + 1) * threads < ((uint64_t)1 << 32); }
-
 static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t s)
 {
     if (a.r.rows == 0) return hipSuccess;
@@ -867,7 +875,6 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
         const int few = pieces >= 12288 ? 1024 : pieces >= 6144 ? 512 : 256, many = pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256;
         const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 256 ? few : a.r.rows <= 512 ? 256 : many);
-        if (!fits(a.r.rows, (int)block.x)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
     }
     return hipGetLastError();
@@ -883,11 +890,10 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         BY_TYPE(type, launch_lanes, DO_GRADIENT, false)(f, l, lane_grid(f, a.r.rows) + more, s);
     } else {
         // short rows: a wavefront each, so that more of them are on their way
-        if (!fits(a.r.rows, WG)) return hipErrorInvalidConfiguration;
         const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
         auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
                        : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
-        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 4 us)
+        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 3.2 us)
         GradArgs b = a;
         const int64_t rounds = a.r.V / ((type == ANAKIN_TYPE_FP32 ? 4 : 8) * 4 * WG);
         b.shares = brief || a.r.rows >= 1024 || rounds < 2 ? 1 : (int)(1024 / (a.r.rows > 0 ? a.r.rows : 1) < rounds ? 1024 / (a.r.rows > 0 ? a.r.rows : 1) : rounds);
@@ -925,7 +931,6 @@ static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipSt
         BY_TYPE(type, launch_lanes, DO_POLICY, false)(f, l, grid, s);
     } else {
         *parts = (int)a.r.rows;
-        if (!fits(a.r.rows, a.r.V > (type == ANAKIN_TYPE_FP32 ? 32768 : 65536) ? 1024 : 512)) return hipErrorInvalidConfiguration;
         if (a.p.ent != 0.0) BY_TYPE(type, launch_block_policy, true)(a, s);
         else BY_TYPE(type, launch_block_policy, false)(a, s);
     }
