@@ -580,11 +580,12 @@ __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// The clipped loss over long rows: a workgroup of NT threads holds a row in registers, VPT pieces of 16 bytes a thread, from
-// the one read to the one write; of a row longer than that the rest is read again.  (Nine pieces more a thread in LDS gained 3 to
-// 5 % on fp32 rows of 100000 to 262144 columns and lost 1 % on bf16 ones of 200000: the second read comes from the caches.)
+// The clipped loss over long rows: a workgroup of NT threads holds a row, VPT pieces of 16 bytes a thread in registers and LPT in
+// LDS, from the one read to the one write; of a row longer than that the rest is read again, from the caches.  The pieces in LDS
+// are loaded there past the registers, which have no room for them even for a moment (through registers 15 were spilled, and half
+// of the gain was lost).
 // ---------------------------------------------------------------------------
-template <class E, int NT, int VPT, bool ENT>
+template <class E, int NT, int VPT, int LPT, bool ENT>
 __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_policy(const PolicyArgs a)
 {
     typedef typename E::T T;
@@ -592,6 +593,9 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
     __shared__ Part lds[WAVES];
     __shared__ double weights[WAVES];
     __shared__ RowGrad row_grad;
+    typedef uint32_t u32x4_whole __attribute__((ext_vector_type(4)));
+    __shared__ u32x4_whole stash[LPT > 0 ? LPT : 1][LPT > 0 ? NT : 1];       // (a thread reads back what it loaded itself)
+    constexpr int HELD = VPT + LPT;
     const int64_t n = blockIdx.x;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int target = policy_target(a, n);
@@ -615,6 +619,11 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
     const float chosen = E::get(row + target);
     u32x4_any w[VPT];
 #pragma unroll
+    for (int k = 0; k < LPT; ++k)                                      // (lane l of a wavefront at 16 l bytes)
+        if (tid + (VPT + k) * NT < cut.pieces)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(in + (int64_t)(tid + (VPT + k) * NT) * E::N),
+                                             (__attribute__((address_space(3))) void*)&stash[k][__builtin_amdgcn_readfirstlane(wave) * 64], 16, 0, 0);
+#pragma unroll
     for (int k = 0; k < VPT; ++k)
         if (tid + k * NT < cut.pieces) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(tid + k * NT) * E::N);
     const int j_loose = loose_column<E>(cut, tid);
@@ -623,6 +632,10 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
     // maximum of the wavefront's pieces, then their sums at that shift
     const float c = a.r.c, c_lo = a.r.c_lo;
     float m = z_loose;
+    if (LPT > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < LPT; ++k)
+        if (tid + (VPT + k) * NT < cut.pieces) { float z[E::N]; E::unpack(stash[k][tid], z); m = max_of(z, m); }
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
         if (tid + k * NT < cut.pieces) { float z[E::N]; E::unpack(w[k], z); m = max_of(z, m); }
@@ -632,8 +645,11 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
         if (tid + k * NT < cut.pieces) { float z[E::N]; E::unpack(w[k], z); add_at<false>(p, z, 0.0f, s, c, c_lo); }
+#pragma unroll
+    for (int k = 0; k < LPT; ++k)
+        if (tid + (VPT + k) * NT < cut.pieces) { float z[E::N]; E::unpack(stash[k][tid], z); add_at<false>(p, z, 0.0f, s, c, c_lo); }
     if (tid < cut.loose) { const float z[1] = {z_loose}; add_at<false>(p, z, 0.0f, s, c, c_lo); }
-    for (int v = tid + VPT * NT; v < cut.pieces; v += NT) {
+    for (int v = tid + HELD * NT; v < cut.pieces; v += NT) {
         float z[E::N];
         E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
         add_elements<false>(p, z, c, c_lo);
@@ -664,7 +680,10 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
         if (tid + k * NT < cut.pieces) put_piece<E, ENT>(q, w[k], to + (int64_t)(tid + k * NT) * E::N);
-    for (int v = tid + VPT * NT; v < cut.pieces; v += NT) put_piece<E, ENT>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
+#pragma unroll
+    for (int k = 0; k < LPT; ++k)
+        if (tid + (VPT + k) * NT < cut.pieces) put_piece<E, ENT>(q, stash[k][tid], to + (int64_t)(tid + (VPT + k) * NT) * E::N);
+    for (int v = tid + HELD * NT; v < cut.pieces; v += NT) put_piece<E, ENT>(q, *reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), to + (int64_t)v * E::N);
     if (tid < cut.loose) put_element<E, ENT>(q, z_loose, 0.0f, out + j_loose);
     if (stores_target<E, NT>(cut, target)) put_element<E, ENT>(q, chosen, q.to_target, out + target);
 }
@@ -906,16 +925,23 @@ static void launch_block_policy(const PolicyArgs& a, hipStream_t s)
 {
     // As few threads as hold a row: several rows share a compute unit, and one is loaded while another is added up.  GB/s read and
     // written (bf16) with these and with 1024 threads: 16384 x 12000 5000 and 1970, 16384 x 32768 5740 and 4250, 4096 x 65536 4800
-    // and 4250; 65536 x 2500 with 128 threads 4030, with 256 2600.  Beyond 1024 threads of 16 pieces the rest is read twice.
+    // and 4250; 65536 x 2500 with 128 threads 4030, with 256 2600.
+    // Two rows of 29 pieces a thread fit a compute unit with 9 of them in LDS; where rows are fewer than that one of 1024 threads
+    // is faster (us: fp32 512 x 50001 42 and 50, 256 x 50001 29 and 27; bf16 4096 x 100003 343 and 368, 1125 x 100003 119 and 134).
+    // Three rows of 10 pieces in registers and 6 in LDS in place of two of 16 are not (bf16 4096 x 65536 243 and 224).
+    // Longer rows: 16 pieces, and 9 in LDS, of 1024 threads, the rest read twice (without those 9: bf16 2048 x 200000 365 and 393,
+    // fp32 256 x 100003 45 and 52).
     const int64_t pieces = (a.r.V + E::N - 1) / E::N;
     const dim3 grid((unsigned)a.r.rows);
-    if (pieces <= 64 * 4) hipLaunchKernelGGL((block_policy<E, 64, 4, ENT>), grid, dim3(64), 0, s, a);
-    else if (pieces <= 128 * 4) hipLaunchKernelGGL((block_policy<E, 128, 4, ENT>), grid, dim3(128), 0, s, a);
-    else if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, ENT>), grid, dim3(256), 0, s, a);
-    else if (pieces <= 256 * 8) hipLaunchKernelGGL((block_policy<E, 256, 8, ENT>), grid, dim3(256), 0, s, a);
-    else if (pieces <= 512 * 8) hipLaunchKernelGGL((block_policy<E, 512, 8, ENT>), grid, dim3(512), 0, s, a);
-    else if (pieces <= 512 * 16) hipLaunchKernelGGL((block_policy<E, 512, 16, ENT>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((block_policy<E, 1024, 16, ENT>), grid, dim3(1024), 0, s, a);
+    if (pieces <= 64 * 4) hipLaunchKernelGGL((block_policy<E, 64, 4, 0, ENT>), grid, dim3(64), 0, s, a);
+    else if (pieces <= 128 * 4) hipLaunchKernelGGL((block_policy<E, 128, 4, 0, ENT>), grid, dim3(128), 0, s, a);
+    else if (pieces <= 256 * 4) hipLaunchKernelGGL((block_policy<E, 256, 4, 0, ENT>), grid, dim3(256), 0, s, a);
+    else if (pieces <= 256 * 8) hipLaunchKernelGGL((block_policy<E, 256, 8, 0, ENT>), grid, dim3(256), 0, s, a);
+    else if (pieces <= 512 * 8) hipLaunchKernelGGL((block_policy<E, 512, 8, 0, ENT>), grid, dim3(512), 0, s, a);
+    else if (pieces <= 512 * 16) hipLaunchKernelGGL((block_policy<E, 512, 16, 0, ENT>), grid, dim3(512), 0, s, a);
+    else if (pieces <= 512 * 29 && a.r.rows > 256) hipLaunchKernelGGL((block_policy<E, 512, 20, 9, ENT>), grid, dim3(512), 0, s, a);
+    else if (pieces <= 1024 * 16) hipLaunchKernelGGL((block_policy<E, 1024, 16, 0, ENT>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((block_policy<E, 1024, 16, 9, ENT>), grid, dim3(1024), 0, s, a);
 }
 // *parts: how many workgroups report sums
 static hipError_t launch_policy(int type, const PolicyArgs& a, int* parts, hipStream_t s)

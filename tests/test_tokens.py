@@ -609,6 +609,42 @@ def test_rows_that_begin_anywhere(dtype, V, begin, to):
 
 
 @gpu
+@pytest.mark.parametrize("rows,dtype,V", [(257, "fp32", 32769), (300, "fp32", 50001), (300, "fp32", 59392), (300, "fp32", 59399), (257, "bf16", 65537), (300, "fp16", 100003), (300, "bf16", 118791),
+                                          (20, "fp32", 50001), (20, "fp32", 65600), (20, "fp32", 102400), (20, "fp32", 102411), (20, "bf16", 131080), (20, "fp16", 204800), (20, "bf16", 220007)])
+def test_long_rows_of_the_clipped_loss(rows, dtype, V):
+    """Rows on both sides of what registers and LDS hold, targets in every part of them; in place and not are alike; two calls too."""
+    z, t, g = make_logits(12, V, dtype, seed=8)
+    z[:, ::97] = -math.inf
+    t = torch.tensor([1, 5, V - 1, V - 2, V // 2, 16384, V * 3 // 4, V - 600, 60, V // 3, V - 5000, 20001], device="cuda")
+    z[torch.arange(12, device="cuda"), t] = 1.0
+    at = torch.arange(12, device="cuda") * (rows // 13) + 1
+    stride = V + 3
+    buf = torch.full((rows * stride,), math.nan, dtype=DT[dtype], device="cuda")
+    zb = buf.as_strided((rows, V), (stride, 1))
+    zb[at] = z.cuda()
+    tg = torch.full((rows,), -1, device="cuda")
+    tg[at] = t
+    x = ref_rows(z.cuda(), t, 1.0)
+    adv = torch.randn(12, generator=g)
+    old, ref = (x["lp"] - 0.05 * torch.randn(12, generator=g)).float(), (x["lp"] + 0.3).float()
+    spread = lambda v: torch.zeros(rows, device="cuda").index_copy(0, at, v.cuda())
+    call = lambda out=None: tokens.policy_loss(zb, tg, spread(old), spread(adv), kl_coef=0.1, logp_ref=spread(ref), entropy_coef=0.02, out=out)
+    p, again = call(), call()
+    stats, g1, g2, on, size = ref_policy(x, old, adv, 0.2, 0.2, 0.1, ref, 0.02, None, 0.0)
+    close_gradient(p.dlogits[at], ref_gradient(x, g1, g2, 1.0)[0], 3 * ref_gradient(x, size, g2, 1.0)[1], V, DT[dtype])
+    close(p.logp[at], x["lp"], U * x["lp"].abs() + 2 * roundings(V), "logp")
+    close(p.stats, torch.tensor(stats, dtype=torch.float64), 4 * (1 + torch.tensor(stats).double().abs() + 3) * roundings(V), "stats")
+    off = torch.ones(rows, dtype=torch.bool, device="cuda")
+    off[at] = False
+    assert not p.dlogits[off].any() and not p.logp[off].any()
+    assert torch.equal(p.dlogits, again.dlogits) and torch.equal(p.stats, again.stats)
+    q = call(out=zb)
+    assert torch.equal(q.dlogits, p.dlogits) and torch.equal(q.stats, p.stats)
+    gaps = buf.as_strided((rows - 1, 3), (stride, 1), V)
+    assert torch.isnan(gaps).all()
+
+
+@gpu
 @pytest.mark.parametrize("V", [6, 300, 9000])
 def test_a_pair_with_an_impossible_token(V):
     """A forbidden target, and a row that allows nothing: the log-probability of their sequence is minus infinity; the gradient stays
