@@ -477,7 +477,23 @@ __device__ __forceinline__ Sums block_joined(Part p, float c, float c_lo, Part* 
     rescale<FINE>(p, m, c, c_lo);
     return Sums{m, block_sum(fma(LN2, (double)p.u, (double)p.s), lds_s), 0.0};
 }
-template <class E, bool FINE>
+// U pieces of this thread, all loaded before the first is used
+template <class E, bool FINE, int U>
+__device__ __forceinline__ void add_pieces(Part& p, const typename E::T* in, int v, int nt, float c, float c_lo)
+{
+    u32x4_any w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * nt) * E::N);
+    float z[U][E::N], m = p.m;
+#pragma unroll
+    for (int k = 0; k < U; ++k) { E::unpack(w[k], z[k]); m = max_of(z[k], m); }
+    if (m > p.m) rescale<FINE>(p, m, c, c_lo);
+    const Shift s = shift_of(m, c);
+    const float m0 = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int k = 0; k < U; ++k) add_at<FINE>(p, z[k], m0, s, c, c_lo);
+}
+template <class E, bool FINE, int U>                                   // U: loads in flight
 __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
 {
     __shared__ Part lds[16];
@@ -489,24 +505,12 @@ __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
     Part p{-INFINITY, 0.0f, 0.0f};
     Sums sums{};
     if (target >= 0) {
-        constexpr int U = 4;                                            // loads in flight
         const Cut cut = cut_at<E>(row, V);
         const typename E::T* in = row + cut.head;
         const float c = a.r.c, c_lo = a.r.c_lo;
         int v = threadIdx.x;
-        for (; v + (U - 1) * nt < cut.pieces; v += U * nt) {
-            u32x4_any w[U];
-#pragma unroll
-            for (int k = 0; k < U; ++k) w[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)(v + k * nt) * E::N);
-            float z[U][E::N], m = p.m;
-#pragma unroll
-            for (int k = 0; k < U; ++k) { E::unpack(w[k], z[k]); m = max_of(z[k], m); }
-            if (m > p.m) rescale<FINE>(p, m, c, c_lo);
-            const Shift s = shift_of(m, c);
-            const float m0 = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int k = 0; k < U; ++k) add_at<FINE>(p, z[k], m0, s, c, c_lo);
-        }
+        for (; v + (U - 1) * nt < cut.pieces; v += U * nt) add_pieces<E, FINE, U>(p, in, v, nt, c, c_lo);
+        if (U > 4 && v + 3 * nt < cut.pieces) { add_pieces<E, FINE, 4>(p, in, v, nt, c, c_lo); v += 4 * nt; }
         for (; v < cut.pieces; v += nt) {
             float z[E::N];
             E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
@@ -914,7 +918,11 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
         const int few = pieces >= 12288 ? 1024 : pieces >= 6144 ? 512 : 256, many = pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256;
         const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 256 ? few : a.r.rows <= 512 ? 256 : many);
-        hipLaunchKernelGGL(fine ? BY_TYPE(type, block_sums, true) : BY_TYPE(type, block_sums, false), grid, block, 0, s, a);
+        // Loads in flight of a thread: 8, but for rows of a wavefront, where more wavefronts to a compute unit are worth more (us with 4 and
+        // 8, bf16: 4096 x 65536 101.7 and 97.4, 16384 x 16384 100 and 94; 32768 x 6000 84 and 86, 65536 x 2500 80 and 93).
+        auto k = pieces <= 1024 ? (fine ? BY_TYPE(type, block_sums, true, 4) : BY_TYPE(type, block_sums, false, 4))
+                                : (fine ? BY_TYPE(type, block_sums, true, 8) : BY_TYPE(type, block_sums, false, 8));
+        hipLaunchKernelGGL(k, grid, block, 0, s, a);
     }
     return hipGetLastError();
 }
