@@ -568,6 +568,8 @@ __device__ __forceinline__ bool stores_target(const Cut& cut, int target)
 // last to the first and the gradient is stored past the caches (6000 x 100003 fp16, all of the loss: 638 us without either, 645
 // and 638 with one of them, 614 with both).
 // ---------------------------------------------------------------------------
+// (us with 4 and 8: 6000 x 100003 fp16 508 and 496, 4096 x 50001 fp32 345 and 337; 65536 x 2500 bf16, a wavefront each, 124 and 137)
+constexpr int loads_in_flight(int threads) { return threads > 64 ? 8 : 4; }
 template <class E, bool ENT, bool AGAIN, int NT>
 __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
 {
@@ -578,7 +580,7 @@ __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
     const RowGrad q = grad_of_row(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
-    constexpr int U = 4;
+    constexpr int U = loads_in_flight(NT);
     const int share = (int)(blockIdx.x % a.shares);                     // of the row, in whole rounds of U pieces a thread
     if (q.target < 0) { if (share == 0) zero_row<E, NT>(out, a.r.V); return; }
     const Cut cut = cut_at<E>(row, a.r.V);
@@ -940,9 +942,9 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
         auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
                        : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
-        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 3.2 us)
+        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 3.5 us)
         GradArgs b = a;
-        const int64_t rounds = a.r.V / ((type == ANAKIN_TYPE_FP32 ? 4 : 8) * 4 * WG);
+        const int64_t rounds = a.r.V / ((type == ANAKIN_TYPE_FP32 ? 4 : 8) * loads_in_flight(WG) * WG);
         b.shares = brief || a.r.rows >= 1024 || rounds < 2 ? 1 : (int)(1024 / (a.r.rows > 0 ? a.r.rows : 1) < rounds ? 1024 / (a.r.rows > 0 ? a.r.rows : 1) : rounds);
         hipLaunchKernelGGL(k, dim3((unsigned)(a.r.rows * b.shares) + more), dim3(brief ? 64 : WG), 0, s, b);
     }
