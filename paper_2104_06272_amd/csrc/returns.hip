@@ -10,7 +10,7 @@
 // returns_columns: time-major; up to 32 columns (128 bytes: whole cache lines) by as many pieces of 8 steps as 1024 threads
 // make, 256 steps with 32 columns.
 // Where the maps of other workgroups are needed they come from a first launch of the same kernel that only composes
-// (APPLY false).  Columns that fill the device by themselves walk their tiles one after another in one launch instead.
+// (APPLY false); where they are many, carry_maps composes them in between.  Columns that fill the device by themselves walk their tiles one after another in one launch instead.
 #include <math.h>
 #include <initializer_list>
 #include "tokens.h"
@@ -35,6 +35,7 @@ struct ReturnsArgs {
     int tiles;                                   // of the rows, or of the time axis
     int width; unsigned groups;                  // columns: of a workgroup, and how many such groups
     int walk;                                    // columns: one workgroup takes all tiles of its columns in turn
+    int carried;                                 // a tile's map is that of all tiles behind it (carry_maps)
 };
 
 // The map of everything behind this thread's piece in its column of the workgroup (threads piece * W + column), and of the
@@ -60,6 +61,28 @@ __device__ __forceinline__ void block_maps(const Map& own, int W, Map* lds, Map&
     if (!WHOLE) return;
     whole = lds[col];
     for (int w = 1; w < waves && whole.a != 0.0; ++w) whole = composed(whole, lds[w * W + col]);
+}
+
+// In place of every tile's map that of everything behind the tile: each tile would compose them by itself otherwise, which is
+// quadratic in their number.  W columns a workgroup; a thread takes a run of tiles of one column, from the last to the first.
+__global__ __launch_bounds__(COLS_WG) void carry_maps(Map* maps, const int tiles, const int64_t S, const int W)
+{
+    __shared__ Map lds[(COLS_WG / 64) * COLS_MAX];
+    const int piece = threadIdx.x / W, pieces = blockDim.x / W, per = (tiles + pieces - 1) / pieces;
+    const int64_t col = (int64_t)blockIdx.x * W + threadIdx.x % W;
+    const int first = piece * per < tiles ? piece * per : tiles, end = first + per < tiles ? first + per : tiles, n = col < S ? end - first : 0;
+    Map own{1.0, 0.0};
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) own = composed(own, maps[(int64_t)(first + k) * S + col]);
+    Map behind, whole;
+    block_maps<false>(own, W, lds, behind, whole);
+#pragma unroll 8
+    for (int k = n - 1; k >= 0; --k) {
+        const int64_t i = (int64_t)(first + k) * S + col;
+        const Map m = maps[i];
+        maps[i] = behind;
+        behind = composed(m, behind);
+    }
 }
 
 template <class E>
@@ -161,7 +184,8 @@ __global__ __launch_bounds__(WG) void returns_rows(const ReturnsArgs a)
     }
     // what reaches the end of this tile: the maps of the tiles behind it, 64 at a time until one of them cuts
     Map later{1.0, 0.0};
-    for (int64_t base = (int64_t)blockIdx.x + 1; base < gridDim.x && later.a != 0.0; base += 64) {
+    if (a.carried) later = a.maps[blockIdx.x];
+    else for (int64_t base = (int64_t)blockIdx.x + 1; base < gridDim.x && later.a != 0.0; base += 64) {
         const int64_t t = base + (threadIdx.x & 63);
         Map c = t < gridDim.x ? a.maps[t] : Map{0.0, 0.0};             // nothing behind the last row
         for (int dist = 1; dist < 64; dist <<= 1) {
@@ -218,7 +242,8 @@ __global__ __launch_bounds__(COLS_WG) void returns_columns(const ReturnsArgs a)
     Map later{1.0, 0.0};                                               // of the tiles behind
     Steps next;
     load_column<E>(a, my_tile * tile_steps + (int64_t)piece * STEPS, n, col, next);
-    if (APPLY && !a.walk && a.tiles > 1) {
+    if (APPLY && a.carried) { if (mine) later = a.maps[my_tile * S + col]; }
+    else if (APPLY && !a.walk && a.tiles > 1) {
         // of the other workgroups' maps: every piece takes its share of the tiles behind this one
         const int64_t rest = a.tiles - 1 - my_tile, per = (rest + pieces - 1) / pieces, t0 = my_tile + 1 + piece * per;
         Map c{1.0, 0.0}, behind;
@@ -272,6 +297,16 @@ static ColumnForm column_form(int64_t count, int64_t length)
     return f;
 }
 
+// A tile looks at the maps behind it in rounds, of 64 of them or of as many as a column has pieces; above so many rounds a launch
+// more that looks at them once is faster (us without and with: one sequence of 2^21 tokens 32 and 31, of 2^22 72 and 37, of 2^26 9600
+// and 380; time-major, 64 columns: 2^22 tokens 42 and 45, 2^24 243 and 131; 1024 columns, 2^26 tokens 611 and 487)
+constexpr int CARRY_FROM = 16;
+static hipError_t launch_carry(const ReturnsArgs& a, int64_t columns, int W, hipStream_t s)
+{
+    hipLaunchKernelGGL(carry_maps, dim3((unsigned)((columns + W - 1) / W)), dim3(COLS_WG), 0, s, a.maps, a.tiles, columns, W);
+    return hipGetLastError();
+}
+
 template <class E>
 static hipError_t launch_returns_of(ReturnsArgs& a, hipStream_t s)
 {
@@ -281,7 +316,9 @@ static hipError_t launch_returns_of(ReturnsArgs& a, hipStream_t s)
         const dim3 grid(a.groups * (f.walk ? 1u : (unsigned)f.tiles)), block(f.width * f.pieces);
         if (!f.walk && f.tiles > 1) {
             hipLaunchKernelGGL((returns_columns<E, false>), grid, block, 0, s, a);
-            const hipError_t e = hipGetLastError();
+            hipError_t e = hipGetLastError();
+            a.carried = f.tiles > CARRY_FROM * f.pieces;
+            if (e == hipSuccess && a.carried) e = launch_carry(a, a.q.count, f.width, s);
             if (e != hipSuccess) return e;
         }
         hipLaunchKernelGGL((returns_columns<E, true>), grid, block, 0, s, a);
@@ -290,7 +327,9 @@ static hipError_t launch_returns_of(ReturnsArgs& a, hipStream_t s)
     a.tiles = (int)((a.q.rows + ROWS_TILE - 1) / ROWS_TILE);
     if (a.tiles > 1) {
         hipLaunchKernelGGL((returns_rows<E, false>), dim3(a.tiles), dim3(WG), 0, s, a);
-        const hipError_t e = hipGetLastError();
+        hipError_t e = hipGetLastError();
+        a.carried = a.tiles > CARRY_FROM * 64;
+        if (e == hipSuccess && a.carried) e = launch_carry(a, 1, 1, s);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((returns_rows<E, true>), dim3(a.tiles), dim3(WG), 0, s, a);

@@ -645,6 +645,38 @@ def test_long_rows_of_the_clipped_loss(rows, dtype, V):
 
 
 @gpu
+@pytest.mark.parametrize("layout,count,length", [("packed", 1, 2100000), ("packed", 1, 2097153), ("packed", 3, 1500000), ("batch", 2, 1100001), ("batch", 1, 5000000), ("time", 1, 2200000),
+                                                 ("time", 2, 2100000), ("time", 7, 600000), ("time", 33, 33000), ("time", 40, 50001), ("time", 300, 35000)])
+def test_very_long_sequences(layout, count, length):
+    """gamma = lambda = 1 and numbers of 1/1024: every sum is exact in 64 bits, so returns and advantages are the rounded exact ones."""
+    g = torch.Generator().manual_seed(count)
+    N = count * length
+    r, v = (torch.randint(-2048, 2049, (N,), generator=g) / 1024 for _ in range(2))
+    done = (torch.rand(N, generator=g) < 2.0 / length).to(torch.uint8)
+    boot = torch.randint(-2048, 2049, (count,), generator=g) / 1024
+    lengths = torch.full((count,), length, dtype=torch.int32)
+    if count > 1:
+        lengths[0], lengths[1] = length - 777, length // 2
+    if layout == "packed":
+        seq = tokens.packed(torch.tensor([0] + lengths.cumsum(0).tolist(), device="cuda"))
+    else:
+        seq = (tokens.batch_major if layout == "batch" else tokens.time_major)(count, length, lengths.cuda())
+    adv, ret = tokens.lambda_returns(r.cuda(), v.cuda(), seq, gamma=1.0, lam=1.0, done=done.cuda(), bootstrap=boot.cuda())
+    want, member = torch.zeros(N, dtype=torch.float64), torch.zeros(N, dtype=torch.bool)
+    for s, rows in enumerate(rows_of(layout, count, length, lengths.tolist())):
+        x, d = r[rows].double(), done[rows].bool()
+        member[rows] = True
+        ends = (torch.nonzero(d)[:, 0] + 1).tolist()
+        at = 0
+        for e in ends + [len(rows)]:
+            part = torch.flip(torch.cumsum(torch.flip(x[at:e], [0]), 0), [0])
+            want[rows[at:e]] = part + (0.0 if e in ends else float(boot[s]))
+            at = e
+    assert torch.equal(ret.cpu(), want.float())
+    assert torch.equal(adv.cpu(), torch.where(member, want - v.double(), 0.0).float())
+
+
+@gpu
 @pytest.mark.parametrize("V", [6, 300, 9000])
 def test_a_pair_with_an_impossible_token(V):
     """A forbidden target, and a row that allows nothing: the log-probability of their sequence is minus infinity; the gradient stays
