@@ -130,25 +130,22 @@ __device__ __forceinline__ Shift shift_of(float m, float c)
 // of log-probabilities are summed and two such sums subtracted.  Elements of minus infinity add 0 (their t or r enters u
 // clamped); a NaN stays in s.
 struct Part { float m, s, u; };
+// what t changes by from one maximum to a larger one
+__device__ __forceinline__ float step_between(float from, float to, float c)
+{
+    return fmaxf(is_far(from, c) || is_far(to, c) ? (from - to) * c : from * c - to * c, T_MIN);
+}
 template <bool FINE>
 __device__ __forceinline__ void rescale(Part& p, float m, float c, float c_lo)      // to a larger maximum
 {
     if (p.m == m || p.m == -INFINITY) { p.m = m; return; }
-    const float x = p.m - m;
     float d, r = 0.0f;
-    if (FINE) { d = fmaxf(x * c, T_MIN); r = __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -d)), -1.0f, 1.0f); }
-    else d = fmaxf(is_far(p.m, c) || is_far(m, c) ? x * c : p.m * c - m * c, T_MIN);
+    if (FINE) { const float x = p.m - m; d = fmaxf(x * c, T_MIN); r = __builtin_amdgcn_fmed3f(fmaf(x, c_lo, fmaf(x, c, -d)), -1.0f, 1.0f); }
+    else d = step_between(p.m, m, c);
     const float f = __builtin_amdgcn_exp2f(d);
     p.u = f * fmaf(p.s, FINE ? r : d, p.u);
     p.s *= f;
     p.m = m;
-}
-template <bool FINE>
-__device__ __forceinline__ Part joined(Part a, Part b, float c, float c_lo)
-{
-    const float m = fmaxf(a.m, b.m);
-    rescale<FINE>(a, m, c, c_lo); rescale<FINE>(b, m, c, c_lo);
-    return Part{m, a.s + b.s, a.u + b.u};
 }
 // elements at shift k (coarse) or maximum m (fine); s grows by their sum, which is a tree: a thread of a long row adds a few
 // dozen times and not a few hundred
@@ -188,12 +185,6 @@ __device__ __forceinline__ void add_elements(Part& p, const float (&z)[N], float
     if (m > p.m) rescale<FINE>(p, m, c, c_lo);
     add_at<FINE>(p, z, m == -INFINITY ? 0.0f : m, shift_of(m, c), c, c_lo);
 }
-template <bool FINE>
-__device__ __forceinline__ Part lanes_joined(Part p, float c, float c_lo, int lanes)
-{
-    for (int off = 1; off < lanes; off <<= 1) p = joined<FINE>(p, Part{__shfl_xor(p.m, off, 64), __shfl_xor(p.s, off, 64), __shfl_xor(p.u, off, 64)}, c, c_lo);
-    return p;
-}
 
 // ---- one row's numbers in 64 bits --------------------------------------------------------------------------------
 __device__ __forceinline__ double reciprocal(double x)
@@ -226,8 +217,8 @@ __device__ __forceinline__ float exp_of(double x)
     return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(t - i)), (int)i);
 }
 
-// A row's sums as its workgroup or its lanes have them together: `fine` ones are joined in 64 bits, since the roundings of
-// the last few additions in 32 would be most of what is left (u is in s then).
+// A row's sums as its workgroup or its lanes have them together, joined in 64 bits where they are long or `fine`: the roundings of
+// the last few additions in 32 would be most of what is left (of `fine` ones u is in s then).
 struct Sums { float m; double s, u; };
 
 struct RowSum {

@@ -456,18 +456,39 @@ __global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_ro
 // ---------------------------------------------------------------------------
 // Long rows, a workgroup each.  Sums: one pass with every thread's own running maximum; bound by the read.
 // ---------------------------------------------------------------------------
-// (lane 0 of the first wavefront has the result; the number of wavefronts is a power of two)
+// A wavefront's sums at its maximum, and those of a workgroup's wavefronts (a power of two of them) for the lanes of one.  Joined in
+// 64 bits: the roundings of the last ten additions in 32 were most of what a log-probability was off by.
+__device__ __forceinline__ Sums wave_joined(Part p, float c, float c_lo)
+{
+    float m = p.m;
+    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    rescale<false>(p, m, c, c_lo);
+    return Sums{m, wave_sum((double)p.s), wave_sum((double)p.u)};
+}
+__device__ __forceinline__ Sums waves_joined(const Sums* lds, int waves, int lane, float c)
+{
+    Sums q = lds[lane < waves ? lane : 0];
+    float m = q.m;
+    for (int off = 1; off < waves; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    if (q.m != m && q.m != -INFINITY) {
+        const float d = step_between(q.m, m, c);
+        const double f = (double)__builtin_amdgcn_exp2f(d);
+        q.u = f * fma(q.s, (double)d, q.u);
+        q.s *= f;
+    }
+    for (int off = 1; off < waves; off <<= 1) { q.s += __shfl_xor(q.s, off, 64); q.u += __shfl_xor(q.u, off, 64); }
+    return Sums{m, q.s, q.u};
+}
+// (lane 0 of the first wavefront has the result)
 template <bool FINE>
-__device__ __forceinline__ Sums block_joined(Part p, float c, float c_lo, Part* lds, double* lds_s)
+__device__ __forceinline__ Sums block_joined(Part p, float c, float c_lo, Sums* lds, double* lds_s)
 {
     const int waves = blockDim.x >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (!FINE) {
-        p = lanes_joined<FINE>(p, c, c_lo, 64);
-        if (lane == 0) lds[wave] = p;
+        const Sums q = wave_joined(p, c, c_lo);
+        if (lane == 0) lds[wave] = q;
         __syncthreads();
-        if (lane < waves) p = lds[lane];
-        p = lanes_joined<FINE>(p, c, c_lo, waves);
-        return Sums{p.m, (double)p.s, (double)p.u};
+        return waves_joined(lds, waves, lane, c);
     }
     float m = p.m;
     for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
@@ -496,7 +517,7 @@ __device__ __forceinline__ void add_pieces(Part& p, const typename E::T* in, int
 template <class E, bool FINE, int U>                                   // U: loads in flight
 __global__ __launch_bounds__(1024) void block_sums(const SumArgs a)
 {
-    __shared__ Part lds[16];
+    __shared__ Sums lds[16];
     __shared__ double lds_s[16];
     const int64_t n = blockIdx.x;
     const int target = row_target(a.r, n), V = a.r.V, nt = blockDim.x;
@@ -616,7 +637,7 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
 {
     typedef typename E::T T;
     constexpr int WAVES = NT / 64;
-    __shared__ Part lds[WAVES];
+    __shared__ Sums lds[WAVES];
     __shared__ double weights[WAVES];
     __shared__ RowGrad row_grad;
     typedef uint32_t u32x4_whole __attribute__((ext_vector_type(4)));
@@ -680,15 +701,14 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
         E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
         add_elements<false>(p, z, c, c_lo);
     }
-    p = lanes_joined<false>(p, c, c_lo, 64);
-    if (lane == 0) { lds[wave] = p; weights[wave] = share; }
+    const Sums of_wave = wave_joined(p, c, c_lo);
+    if (lane == 0) { lds[wave] = of_wave; weights[wave] = share; }
     __syncthreads();
     if (wave == 0) {
-        p = lds[lane < WAVES ? lane : 0];
-        p = lanes_joined<false>(p, c, c_lo, WAVES);
+        const Sums sums = waves_joined(lds, WAVES, lane, c);
         const double W = wave_sum(lane < WAVES ? weights[lane] : 0.0);
         if (lane == 0) {
-            const RowSum x = finish_row<false>(Sums{p.m, (double)p.s, (double)p.u}, a.r);
+            const RowSum x = finish_row<false>(sums, a.r);
             const double lp = logp_of<false>(x, chosen, a.r), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
             const PolicyRow y = policy_row(a.p, pin, lp, x.entropy, x.empty);
             row_grad = row_gradient(x, y.g * inv, y.e * inv, target, a.r.scale);
