@@ -208,13 +208,17 @@ __device__ __forceinline__ double log_of_sum(double x)
     p = fma(p, g, 1.0 / 5); p = fma(p, g, 1.0 / 3); p = fma(p, g, 1.0);
     return fma((double)e, LN2, 2.0 * f * p);
 }
-// e^x to single precision's last place, for x in 64 bits
-__device__ __forceinline__ float exp_of(double x)
+// e^x, its Taylor series to the 9th power around the nearest power of two (off by 1e-11 of it at most).  (A
+// ratio with the roundings of single precision is what the loss of few rows was off by.)
+__device__ __forceinline__ double exp_of(double x)
 {
     double t = x * LOG2E;
-    t = t > 300.0 ? 300.0 : t < -300.0 ? -300.0 : t;                    // (NaN stays)
-    const double i = rint(t);
-    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(t - i)), (int)i);
+    t = t > 1100.0 ? 1100.0 : t < -1100.0 ? -1100.0 : t;                // infinity and 0 (NaN stays)
+    const double i = rint(t), f = (t - i) * LN2;
+    double p = 1.0 / 362880;
+    p = fma(p, f, 1.0 / 40320); p = fma(p, f, 1.0 / 5040); p = fma(p, f, 1.0 / 720); p = fma(p, f, 1.0 / 120);
+    p = fma(p, f, 1.0 / 24); p = fma(p, f, 1.0 / 6); p = fma(p, f, 0.5); p = fma(p, f, 1.0); p = fma(p, f, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)i);
 }
 
 // A row's sums as its workgroup or its lanes have them together, joined in 64 bits where they are long or `fine`: the roundings of
@@ -240,7 +244,7 @@ __device__ __forceinline__ RowSum finish_row(const Sums& p, const Rows& r)
         x.log_s = log_of_sum(s);
         x.lse = fma(r.scale, (double)p.m, x.log_s);
         // the shift of the gradient: 2^(c z - K) / s' with K = fl(c m)
-        x.inv_s = (float)(reciprocal(s) * (x.far ? 1.0 : (double)exp_of(((double)x.k.K - (double)r.c * (double)p.m) * LN2)));
+        x.inv_s = (float)(reciprocal(s) * (x.far ? 1.0 : exp_of(((double)x.k.K - (double)r.c * (double)p.m) * LN2)));
         return x;
     }
     const double inv = reciprocal(s), mean_t = p.u * inv;               // E[t]

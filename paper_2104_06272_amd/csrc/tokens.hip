@@ -213,7 +213,7 @@ __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
         }
     }
     x.log_s = rest * LN2;
-    x.inv_s = exp_of(-x.log_s);
+    x.inv_s = (float)exp_of(-x.log_s);
     x.entropy = e != 0.0 ? (double)a.entropy[n] : 0.0;
     return row_gradient(x, a.to_logp[n], e, target, a.r.scale);
 }
@@ -239,7 +239,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, const Policy
     PolicyRow x{};
     x.w = (double)in.w;
     if (empty) return x;
-    const double A = in.adv, diff = lp - (double)in.old, r = (double)exp_of(diff);
+    const double A = in.adv, diff = lp - (double)in.old, r = exp_of(diff);
     const bool clipped = (A > 0.0 && diff > a.log_high) || (A < 0.0 && diff < a.log_low);      // (a NaN stays in the gradient)
     x.policy = clipped ? -(A > 0.0 ? a.high : a.low) * A : -r * A;
     x.clipped = clipped ? 1.0 : 0.0; x.ratio = r; x.entropy = entropy;
@@ -253,7 +253,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyCfg& a, const Policy
             p = fma(p, d, 1.0 / 3628800); p = fma(p, d, 1.0 / 362880); p = fma(p, d, 1.0 / 40320); p = fma(p, d, 1.0 / 5040);
             p = fma(p, d, 1.0 / 720); p = fma(p, d, 1.0 / 120); p = fma(p, d, 1.0 / 24); p = fma(p, d, 1.0 / 6); p = fma(p, d, 0.5);
             e2 = p * d * d; e1 = e2 + d;
-        } else { e1 = (double)exp_of(d) - 1.0; e2 = e1 - d; }
+        } else { e1 = exp_of(d) - 1.0; e2 = e1 - d; }
         x.kl = e2;
         if (a.kl != 0.0) x.g -= a.kl * e1;
     }
@@ -780,7 +780,7 @@ __global__ __launch_bounds__(1024) void pair_sums(const PairArgs a)
         if (a.margins && threadIdx.x == 0) a.margins[k] = (float)h;
         __syncthreads();                                                // (sums are read before the next pair's are written)
         if (w == 0.0) continue;
-        const double e = (double)exp_of(-fabs(h)), up = reciprocal(1.0 + e), down = e * up;         // sigmoid(|h|), sigmoid(-|h|)
+        const double e = exp_of(-fabs(h)), up = reciprocal(1.0 + e), down = e * up;         // sigmoid(|h|), sigmoid(-|h|)
         const double soft = e < 1e-4 ? e * (1.0 - 0.5 * e) : log_of_sum(1.0 + e);                   // ln(1 + e^-|h|)
         const double sig = h >= 0.0 ? up : down, gis = h >= 0.0 ? down : up;
         const double dh = w * a.beta * ((1.0 - y) * sig - y * gis) * inv;
