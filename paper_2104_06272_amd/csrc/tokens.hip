@@ -935,13 +935,13 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         if (fine) BY_TYPE(type, launch_lanes, DO_SUMS, true)(f, l, lane_grid(f, a.r.rows), s);
         else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
     } else {
-        // Fewer rows than compute units: 16 pieces a thread (one row of 131072 bf16 with 256 threads 15.4 us, with 1024 12.9; 64 x 8192
-        // 5.3 and 6.9).  Many rows: the shorter they are the fewer threads, so that more of them are on their way.
+        // Fewer rows than compute units: 16 pieces a thread (one row of 131072 bf16 with 256 threads 11.7 us, with 1024 10.2; 64 x 8192
+        // 4.1 and 5.0).  Many rows: the shorter they are the fewer threads, so that more of them are on their way.
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
         const int few = pieces >= 12288 ? 1024 : pieces >= 6144 ? 512 : 256, many = pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256;
         const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 256 ? few : a.r.rows <= 512 ? 256 : many);
         // Loads in flight of a thread: 8, but for rows of a wavefront, where more wavefronts to a compute unit are worth more (us with 4 and
-        // 8, bf16: 4096 x 65536 101.7 and 97.4, 16384 x 16384 100 and 94; 32768 x 6000 84 and 86, 65536 x 2500 80 and 93).
+        // 8, bf16: 4096 x 65536 101.7 and 97.4 (96.4 since), 16384 x 16384 100 and 94; 32768 x 6000 84 and 86, 65536 x 2500 80 and 93).
         auto k = pieces <= 1024 ? (fine ? BY_TYPE(type, block_sums, true, 4) : BY_TYPE(type, block_sums, false, 4))
                                 : (fine ? BY_TYPE(type, block_sums, true, 8) : BY_TYPE(type, block_sums, false, 8));
         hipLaunchKernelGGL(k, grid, block, 0, s, a);
