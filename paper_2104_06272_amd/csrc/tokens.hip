@@ -192,10 +192,14 @@ __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
 {
     RowSum x{};
     if (a.ws) {
+        // (a coefficient of 0 -- a row in no pair, or of a pair of weight 0 -- is a row without a target: its logits, which may
+        // be anything, are not read)
         const RowWs w = a.ws[n];
+        const float g = a.to_logp[n];
+        if (w.target < 0 || g == 0.0f) { RowGrad q{}; q.target = -1; return q; }
         x.k = w.k; x.inv_s = w.inv_s;
         x.empty = w.inv_s == 0.0f;                                      // (all of it minus infinity)
-        return row_gradient(x, a.to_logp[n], 0.0, w.target, a.r.scale);
+        return row_gradient(x, g, 0.0, w.target, a.r.scale);
     }
     const int target = row_target(a.r, n);
     if (target < 0) { RowGrad q{}; q.target = -1; return q; }

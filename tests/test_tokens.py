@@ -793,3 +793,39 @@ def test_python_refusals_on_the_gpu():
     with pytest.raises(binding.AnakinError):                        # overlaps without being the same rows
         tokens.policy_loss(room[:, :6], t, f, f, out=room[:, 1:7])
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("layout", ["packed", "batch", "time"])
+@pytest.mark.parametrize("V", [5, 70, 300, 1031, 5001, 70001])
+def test_rows_outside_the_pairs_may_hold_anything(dtype, layout, V):
+    """Rows in no sequence and rows of pairs of weight 0 get zeros, whatever their logits and references hold; the other rows' gradient
+    and the loss are those of ordinary numbers in their place, in place too."""
+    n, length = [3, 1, 4, 0, 2, 3], 4
+    rows = rows_of(layout, 6, length, n)
+    N = 24 if layout != "packed" else sum(n) + 5
+    if layout == "packed":
+        seq = tokens.packed(torch.tensor([0] + list(np.cumsum(n)), device="cuda"))
+    else:
+        seq = (tokens.batch_major if layout == "batch" else tokens.time_major)(6, length, torch.tensor(n, dtype=torch.int32, device="cuda"))
+    z, room, g = make_logits(N, V, dtype, 1, seed=9)
+    t = make_target(N, V, g)
+    ref, label, weight = torch.randn(N, generator=g).cuda(), torch.rand(3, generator=g).cuda(), torch.tensor([1.0, 0.0, 0.5], device="cuda")
+    on = np.zeros(N, bool)
+    for s in (0, 2, 3, 5):
+        on[rows[s]] = True
+    off = torch.tensor(~on, device="cuda")
+    call = lambda x, r, **kw: tokens.preference_loss(x, t, seq, beta=0.7, logp_ref=r, label=label, weight=weight, **kw)
+    want = call(z, ref)
+    assert not want.dlogits[off].any() and want.dlogits[~off].any()
+    x, bad = room.clone(), ref.clone()
+    bad[off] = math.nan
+    for k, i in enumerate(torch.nonzero(off)[:, 0].tolist()):
+        x[i, :V] = [math.nan, math.inf, -math.inf][k % 3]
+        x[i, k % V] = [math.nan, -math.inf, math.inf, 1.0][k % 4]
+    got = call(x[:, :V], bad)
+    assert torch.equal(got.stats, want.stats) and torch.equal(got.dlogits, want.dlogits)
+    own = x.clone()
+    again = call(own[:, :V], bad, out=own[:, :V])
+    assert torch.equal(again.dlogits, want.dlogits) and torch.equal(again.stats, want.stats) and torch.equal(own[:, V:], x[:, V:])
