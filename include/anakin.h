@@ -404,7 +404,7 @@ typedef struct {
  * null: lp), divided by their number where `mean` is set; h = beta (D_first - D_second) - margin;
  * l = -y log sigmoid(h) - (1 - y) log sigmoid(-h) with y = d_label[pair] in [0, 1], how far the first of the pair is
  * preferred (null: 1); L = sum w l / W over the pairs, W = sum w or `norm`; d_weight null: 1, a pair of weight 0 takes
- * no part.  d_dlogits (null: the loss alone) = grad_scale dL/dlogits; rows in no pair get zeros.
+ * no part; W = 0 gives loss and gradient 0.  d_dlogits (null: the loss alone) = grad_scale dL/dlogits; rows in no pair get zeros.
  * d_stats[8]: L, and weighted means of [h > 0], beta D_first, beta D_second, h; then W, the pairs and the tokens that
  * took part.  d_margins (may be null) [count / 2]: h; d_logp (may be null): lp of every row with a target. */
 typedef struct {

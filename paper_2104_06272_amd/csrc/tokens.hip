@@ -443,7 +443,8 @@ __global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_ro
                     lp = logp_of<false>(y, chosen, r);
                     const PolicyRow z = policy_row(a.p.p, in, lp, y.entropy, y.empty);
                     if (l == 0) add_stats(v, z);
-                    q = row_gradient(y, z.g * inv, z.e * inv, target, r.scale);
+                    if (inv != 0.0) q = row_gradient(y, z.g * inv, z.e * inv, target, r.scale);
+                    else x = LaneRow<E, PIECES>{};                      // no weight, no gradient, of no matter what
                 }
                 if (there && l == 0 && a.p.logp) a.p.logp[n] = (float)lp;
                 if (there && a.p.out) x.template put_gradient<false>(q, static_cast<T*>(a.p.out) + n * a.p.out_stride, cut, V, lanes, l, slots);
@@ -715,7 +716,7 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
             const RowSum x = finish_row<false>(sums, a.r);
             const double lp = logp_of<false>(x, chosen, a.r), inv = W != 0.0 ? a.p.grad_scale / W : 0.0;
             const PolicyRow y = policy_row(a.p, pin, lp, x.entropy, x.empty);
-            row_grad = row_gradient(x, y.g * inv, y.e * inv, target, a.r.scale);
+            row_grad = row_gradient(x, y.g * inv, y.e * inv, inv != 0.0 ? target : -1, a.r.scale);
             if (a.logp) a.logp[n] = (float)lp;
             double v[STATS] = {};
             add_stats(v, y);
@@ -726,6 +727,7 @@ __global__ __launch_bounds__(NT, VPT <= 4 ? 7 : VPT <= 8 ? 5 : 4) void block_pol
     if (!a.out) return;
     __syncthreads();
     const RowGrad q = row_grad;
+    if (q.target < 0) { zero_row<E, NT>(out, a.r.V); return; }          // no weight, no gradient, of no matter what
     T* to = out + cut.head;
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
@@ -787,7 +789,7 @@ __global__ __launch_bounds__(1024) void pair_sums(const PairArgs a)
         const double e = exp_of(-fabs(h)), up = reciprocal(1.0 + e), down = e * up;         // sigmoid(|h|), sigmoid(-|h|)
         const double soft = e < 1e-4 ? e * (1.0 - 0.5 * e) : log_of_sum(1.0 + e);                   // ln(1 + e^-|h|)
         const double sig = h >= 0.0 ? up : down, gis = h >= 0.0 ? down : up;
-        const double dh = w * a.beta * ((1.0 - y) * sig - y * gis) * inv;
+        const double dh = inv != 0.0 ? w * a.beta * ((1.0 - y) * sig - y * gis) * inv : 0.0;    // (no weight, no gradient)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float g = (float)((i == 0 ? dh : -dh) * per[i]);

@@ -829,3 +829,23 @@ def test_rows_outside_the_pairs_may_hold_anything(dtype, layout, V):
     own = x.clone()
     again = call(own[:, :V], bad, out=own[:, :V])
     assert torch.equal(again.dlogits, want.dlogits) and torch.equal(again.stats, want.stats) and torch.equal(own[:, V:], x[:, V:])
+
+
+@gpu
+@pytest.mark.parametrize("V", [5, 70, 300, 1031, 5001, 70001])
+def test_no_weight_means_no_gradient(V):
+    """Weights that cancel: W = 0 gives loss and gradient 0, also where a ratio overflows, a logit is a NaN or a sequence impossible."""
+    N = 8
+    z, _, g = make_logits(N, V, "fp32")
+    t = make_target(N, V, g)
+    w = torch.tensor([1.0, -1.0] * (N // 2), device="cuda")
+    adv = torch.randn(N, generator=g).cuda()
+    old = torch.zeros(N, device="cuda")
+    old[1] = -2e3
+    for poison in (False, True):
+        if poison:
+            z[3, V - 1] = math.nan
+        r = tokens.policy_loss(z, t, old, adv, entropy_coef=0.1, weight=w)
+        assert not r.stats[:7].any() and float(r.stats[7]) == N and not r.dlogits.any()
+        q = tokens.preference_loss(z, t, tokens.batch_major(4, 2), weight=w[:2])
+        assert not q.stats[:6].any() and not q.dlogits.any()
