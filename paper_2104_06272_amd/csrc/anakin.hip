@@ -484,7 +484,7 @@ extern "C" int32_t anakin_create(anakin_t** out, const anakin_env_cfg* env, cons
     h->seed = seed; h->gstep = 0; h->adam_t = 0; h->have_traj = 0; h->mode = 0; h->prof_on = 0; h->traj_packed = 0; h->traj_no_acts = 0;
     h->pathwise = 0; h->metric_blocks = 0;
     h->token_loss = 0; h->clip_low = h->clip_high = 0.2; h->kl_coef = 0.0; h->beta = 0.1; h->pair_label = h->pair_weight = nullptr; h->pair_chunks = 0;
-    h->metric_token = 0; h->metric_chunks = 0;
+    h->metric_token = 0; h->metric_chunks = 0; h->metric_kl = 0.0;
     h->traj_decoupled = 0; h->actor_stream = nullptr; h->actor_stream_owned = 0; h->ev_fork = nullptr; h->ev_join = nullptr;
     h->ws = static_cast<char*>(d_workspace); h->ws_bytes = workspace_bytes;
     h->scratch = nullptr;
@@ -758,7 +758,7 @@ extern "C" int32_t anakin_learn(anakin_t* h)
         const int32_t rc = acting_logprobs(h);
         if (rc != ANAKIN_OK) return rc;
     }
-    h->metric_token = h->token_loss; h->metric_chunks = h->n_updates;
+    h->metric_token = h->token_loss; h->metric_chunks = h->n_updates; h->metric_kl = h->kl_coef;
     if (h->n_updates == 1) {
         int32_t rc = run_update(h, fused_loss);
         if (rc != ANAKIN_OK) return rc;
@@ -1163,7 +1163,7 @@ extern "C" int32_t anakin_get_metrics(anakin_t* h, anakin_metrics* out)
         double policy = 0.0, entropy = 0.0;
         for (int k = 0; k < h->metric_chunks; ++k) {
             const float* v = st.data() + (size_t)k * 8;
-            if (h->metric_token == ANAKIN_PG_CLIPPED) { policy += (double)v[1] + h->kl_coef * (double)v[2]; entropy -= (double)h->net_cfg.entropy_coef * (double)v[3]; }
+            if (h->metric_token == ANAKIN_PG_CLIPPED) { policy += (double)v[1] + h->metric_kl * (double)v[2]; entropy -= (double)h->net_cfg.entropy_coef * (double)v[3]; }
             else policy += (double)v[0];
         }
         out->policy_loss = policy / h->metric_chunks; out->entropy_loss = entropy / h->metric_chunks;

@@ -197,7 +197,8 @@ struct anakin {
     double clip_low, clip_high, kl_coef, beta;   // their coefficients
     const float *pair_label, *pair_weight;       // ANAKIN_PG_PREFERENCE: the caller's, [pair_chunks][B/2] (labels null: by the rewards)
     int pair_chunks;
-    int metric_token, metric_chunks;             // the last update's kind and number of chunks, for the metrics
+    int metric_token, metric_chunks;             // the last update's kind and number of chunks, and its kl_coef, for the metrics
+    double metric_kl;
     int pathwise;                 // policy gradient through the environment instead of the score function (pendulum)
     int traj_decoupled;           // the stored unroll was collected by a decoupled step: behaviour parameters, no activations
     hipStream_t actor_stream;     // decoupled steps: the actor's stream (the caller's, or created on first use), and the fork/join events

@@ -262,3 +262,19 @@ def test_refusals():
         g.step_decoupled()
     assert e.value.code == binding.E_BAD_CONFIG
     g.close()
+
+
+@gpu
+def test_metrics_are_those_of_the_update_made():
+    """Coefficients set between an update and its metrics belong to the next one."""
+    g, _, _ = _warm(_cfg("catch_small", hidden=[64, 64], B=64, T=20, lr=0.01), seed=5)
+    g.set_policy_gradient(binding.PG_CLIPPED)
+    g.set_clip(0.05, 0.08, 0.3)
+    g.set_updates_per_unroll(4, sequential=True)
+    g.learn()
+    want = g.metrics()
+    g.set_clip(0.2, 0.2, 50.0)
+    g.set_preference(0.7)
+    g.set_policy_gradient(binding.PG_SCORE_FUNCTION)
+    assert g.metrics() == want
+    g.close()
