@@ -356,7 +356,8 @@ typedef struct {
 int32_t anakin_token_logprobs(const anakin_rows* x, float* d_logp, float* d_lse, float* d_entropy, void* hip_stream);
 
 /* Its backward pass: dlogits[n][j] = scale (g[n] ([j = target[n]] - p_j) - e[n] p_j (log p_j + entropy[n])) with
- * g = d_grad_logp, e = d_grad_entropy (null: 0; else d_entropy has to be given) and p from the lse of the forward call.
+ * g = d_grad_logp, e = d_grad_entropy (null: 0; else d_entropy has to be given) and p from the lse of the forward call
+ * (where that is 1024 or more in size, down to rows of a type's lowest value, from the row itself: binary32 would hold it too roughly).
  * dlogits has the logits' type, grad_stride elements from row to row; it may be the logits themselves (same pointer and
  * stride), and else must not overlap them.  Rows that take no part get zeros. */
 int32_t anakin_token_logprobs_backward(const anakin_rows* x, const float* d_lse, const float* d_entropy,

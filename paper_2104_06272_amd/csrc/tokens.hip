@@ -188,6 +188,13 @@ struct GradArgs {
     FinishArgs fin;                              // stats not null: a workgroup more finishes the statistics
     int shares;                                  // long rows: workgroups to a row
 };
+// from the row's numbers (all but its entropy) and the caller's coefficients
+__device__ __forceinline__ RowGrad row_gradient_to(const GradArgs& a, int64_t n, RowSum x, int target)
+{
+    const double e = a.to_entropy ? a.to_entropy[n] : 0.0;
+    x.entropy = e != 0.0 ? (double)a.entropy[n] : 0.0;
+    return row_gradient(x, a.to_logp[n], e, target, a.r.scale);
+}
 __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
 {
     RowSum x{};
@@ -203,23 +210,19 @@ __device__ __forceinline__ RowGrad grad_of_row(const GradArgs& a, int64_t n)
     }
     const int target = row_target(a.r, n);
     if (target < 0) { RowGrad q{}; q.target = -1; return q; }
-    // p_j = 2^(c z - K) / s with K = fl(lse log2 e) and the rest of lse in s.  (A log-sum-exp of 2^30 and more has no room for
-    // probabilities: its neighbours are 64 apart.  The maximum's is 1 and nothing overflows.)
-    const double e = a.to_entropy ? a.to_entropy[n] : 0.0, lse = a.lse[n], k = lse * LOG2E, zc = lse / a.r.scale;
-    x.empty = lse == -INFINITY;
-    x.k = Shift{a.r.c, x.empty ? 0.0f : (float)k};
-    double rest = x.empty ? 0.0 : k - (double)x.k.K;
-    if (fabs(k) >= (double)FAR && !x.empty) {
-        rest = 0.0;
-        if (fabs(zc) < 3.4028234663852886e38) {
-            const float m = (float)zc, p = __builtin_amdgcn_ldexpf(1.0f, 24 - ((int)((__float_as_uint(m) >> 23) & 0xff) - 127));
-            x.k = Shift{p, m * p};
-        }
-    }
-    x.log_s = rest * LN2;
+    // p_j = 2^(c z - K) / s with K = fl(lse log2 e) and the rest of lse in s
+    const double k = (double)a.lse[n] * LOG2E;
+    x.k = Shift{a.r.c, (float)k};
+    x.log_s = (k - (double)x.k.K) * LN2;
     x.inv_s = (float)exp_of(-x.log_s);
-    x.entropy = e != 0.0 ? (double)a.entropy[n] : 0.0;
-    return row_gradient(x, a.to_logp[n], e, target, a.r.scale);
+    return row_gradient_to(a, n, x, target);
+}
+// A log-sum-exp in binary32 is off by up to 2^-15 below LSE_MOST, and so is p of itself.  What lies beyond, up to rows of a type's
+// lowest value, whose log-sum-exp has no room for the logarithm of their length or overflows, takes p from the row's own sums.
+constexpr float LSE_MOST = 1024.0f;
+__device__ __forceinline__ bool by_own_sums(const GradArgs& a, int64_t n)
+{
+    return !a.ws && fabsf(a.lse[n]) >= LSE_MOST && row_target(a.r, n) >= 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -394,8 +397,42 @@ struct LaneRow {
     }
 };
 
+// The gradient of a row of by_own_sums, element by element, after the others.  (Beside them, with the row in registers, they would
+// pay for it in registers of their own: a million rows of 256 bf16 260 us, not 215.)
+template <class E>
+__device__ __forceinline__ void lanes_own_sums(const GradArgs& a, int64_t n, int lanes, int l)
+{
+    const int V = a.r.V, target = row_target(a.r, n);
+    const typename E::T* row = static_cast<const typename E::T*>(a.r.logits) + n * a.r.stride;
+    typename E::T* out = static_cast<typename E::T*>(a.out) + n * a.out_stride;
+    Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int j = l; j < V; j += lanes) { const float z[1] = {E::get(row + j)}; add_elements<false>(p, z, a.r.c, a.r.c_lo); }
+    float m = p.m;
+    for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    rescale<false>(p, m, a.r.c, a.r.c_lo);
+    Sums q{m, (double)p.s, (double)p.u};
+    for (int off = 1; off < lanes; off <<= 1) { q.s += __shfl_xor(q.s, off, 64); q.u += __shfl_xor(q.u, off, 64); }
+    const RowGrad g = row_gradient_to(a, n, finish_row<false>(q, a.r), target);
+#pragma unroll 1
+    for (int j = l; j < V; j += lanes) {
+        const float z[1] = {E::get(row + j)};
+        float d[1];
+        gradient_of<true>(g, z, d);
+        E::put(out + j, d[0] + (j == target ? g.to_target : 0.0f));
+    }
+}
+
+// Wavefronts to a SIMD at least.  16-bit gradients: as many as their common rows fit, where lanes_own_sums would have a few registers
+// more (a million rows of 256 bf16 with three wavefronts 258 us, with four 217).
+template <class E, int DO, int PIECES>
+constexpr int lanes_waves()
+{
+    if (DO == DO_GRADIENT && E::N == 8) return PIECES == 4 ? 4 : PIECES == 2 ? 6 : 1;
+    return PIECES == 4 && E::N == 4 ? 4 : 1;
+}
 template <class E, int DO, int PIECES, bool FINE>
-__global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_rows(const LaneArgs<DO> a)
+__global__ __launch_bounds__(WG, (lanes_waves<E, DO, PIECES>())) void lanes_rows(const LaneArgs<DO> a)
 {
     typedef typename E::T T;
     __shared__ FinishLds lds;
@@ -407,6 +444,7 @@ __global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_ro
         if (a.g.fin.stats) grid -= 1;
     }
     double inv = 0.0, v[STATS] = {};
+    bool left = false;                                                  // rows for lanes_own_sums
     if constexpr (DO == DO_POLICY) {
         const double W = block_sum(weight_share(a.p.norm, r, threadIdx.x, WG), lds.weights);
         inv = W != 0.0 ? a.p.p.grad_scale / W : 0.0;
@@ -419,6 +457,7 @@ __global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_ro
         LaneRow<E, PIECES> x{};
         if constexpr (DO == DO_GRADIENT) {
             if (!there) continue;
+            if (by_own_sums(a.g, n)) { left = true; continue; }
             const RowGrad q = grad_of_row(a.g, n);
             if (q.target >= 0) x.load(row, cut, V, lanes, l, slots);
             x.template put_gradient<E::N == 8>(q, static_cast<T*>(a.g.out) + n * a.g.out_stride, cut, V, lanes, l, slots);
@@ -450,6 +489,11 @@ __global__ __launch_bounds__(WG, PIECES == 4 && E::N == 4 ? 4 : 1) void lanes_ro
                 if (there && a.p.out) x.template put_gradient<false>(q, static_cast<T*>(a.p.out) + n * a.p.out_stride, cut, V, lanes, l, slots);
             }
         }
+    }
+    if constexpr (DO == DO_GRADIENT) {
+        if (!left) return;
+        for (int64_t n = (int64_t)blockIdx.x * per + threadIdx.x / lanes; n < r.rows; n += grid * per)
+            if (by_own_sums(a.g, n)) lanes_own_sums<E>(a.g, n, lanes, l);
     }
     if constexpr (DO == DO_POLICY) {
         const int lane = threadIdx.x & 63;
@@ -596,6 +640,8 @@ __device__ __forceinline__ bool stores_target(const Cut& cut, int target)
 // ---------------------------------------------------------------------------
 // (us with 4 and 8: 6000 x 100003 fp16 508 and 496, 4096 x 50001 fp32 345 and 337; 65536 x 2500 bf16, a wavefront each, 124 and 137)
 constexpr int loads_in_flight(int threads) { return threads > 64 ? 8 : 4; }
+// (q lies in scalar registers, whichever way it came)
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 template <class E, bool ENT, bool AGAIN, int NT>
 __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
 {
@@ -603,17 +649,38 @@ __global__ __launch_bounds__(NT) void block_gradients(const GradArgs a)
     __shared__ FinishLds lds;
     if (a.fin.stats && blockIdx.x == gridDim.x - 1) { finish(a.fin, lds); return; }
     const int64_t n = AGAIN ? a.r.rows - 1 - blockIdx.x / a.shares : blockIdx.x / a.shares;
-    const RowGrad q = grad_of_row(a, n);
+    RowGrad q = grad_of_row(a, n);
     const T* row = static_cast<const T*>(a.r.logits) + n * a.r.stride;
     T* out = static_cast<T*>(a.out) + n * a.out_stride;
     constexpr int U = loads_in_flight(NT);
-    const int share = (int)(blockIdx.x % a.shares);                     // of the row, in whole rounds of U pieces a thread
+    int share = (int)(blockIdx.x % a.shares), shares = a.shares;        // of the row, in whole rounds of U pieces a thread
     if (q.target < 0) { if (share == 0) zero_row<E, NT>(out, a.r.V); return; }
     const Cut cut = cut_at<E>(row, a.r.V);
-    const int rounds = (cut.pieces + U * NT - 1) / (U * NT), each = (rounds + a.shares - 1) / a.shares;
-    const int begin = share * each * U * NT, end = begin + each * U * NT < cut.pieces ? begin + each * U * NT : cut.pieces;
     const T* in = row + cut.head;
     T* to = out + cut.head;
+    if (!AGAIN && by_own_sums(a, n)) {
+        // (the first workgroup alone: the gradient may overwrite what others would still add up)
+        if (share != 0) return;
+        shares = 1;
+        __shared__ Sums waves[NT / 64];
+        __shared__ RowGrad own;
+        Part p{-INFINITY, 0.0f, 0.0f};
+        for (int v = threadIdx.x; v < cut.pieces; v += NT) {
+            float z[E::N];
+            E::unpack(*reinterpret_cast<const u32x4_any*>(in + (int64_t)v * E::N), z);
+            add_elements<false>(p, z, a.r.c, a.r.c_lo);
+        }
+        if ((int)threadIdx.x < cut.loose) {
+            const float z[1] = {E::get(row + loose_column<E>(cut, threadIdx.x))};
+            add_elements<false>(p, z, a.r.c, a.r.c_lo);
+        }
+        const Sums sums = block_joined<false>(p, a.r.c, a.r.c_lo, waves, nullptr);
+        if (threadIdx.x == 0) own = row_gradient_to(a, n, finish_row<false>(sums, a.r), q.target);
+        __syncthreads();
+        q = RowGrad{Shift{uniform(own.k.c), uniform(own.k.K)}, uniform(own.a0), uniform(own.a1), uniform(own.to_target), q.target};
+    }
+    const int rounds = (cut.pieces + U * NT - 1) / (U * NT), each = (rounds + shares - 1) / shares;
+    const int begin = share * each * U * NT, end = begin + each * U * NT < cut.pieces ? begin + each * U * NT : cut.pieces;
     // (the target's logit before it is overwritten; of a row in shares, by the one that stores it)
     const int tp = q.target - cut.head, tv = tp >= 0 ? tp / E::N : 0;
     const bool loose = tp < 0 || tv >= cut.pieces, mine = loose ? share == 0 : tv >= begin && tv < end;

@@ -849,3 +849,33 @@ def test_no_weight_means_no_gradient(V):
         assert not r.stats[:7].any() and float(r.stats[7]) == N and not r.dlogits.any()
         q = tokens.preference_loss(z, t, tokens.batch_major(4, 2), weight=w[:2])
         assert not q.stats[:6].any() and not q.dlogits.any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [2, 9, 64, 300, 1030, 5000, 33000, 132000])
+@pytest.mark.parametrize("scale", [1.0, 1.25, 0.7, 0.37])
+def test_backward_pass_of_masks_and_extremes(dtype, V, scale):
+    """Every row of the kinds above, whose log-sum-exp may be past what binary32 tells probabilities from, or past its range."""
+    z, t = _special(dtype, V)
+    g = torch.Generator().manual_seed(2)
+    base = torch.randn(V, generator=g)
+    more = torch.stack([base + o for o in (900.0, -1500.0, 2e4, -6e4 if dtype == "fp16" else -3e7)]).to(DT[dtype])
+    z, t = torch.cat([z, more, more]), torch.cat([t, torch.tensor([0, V - 1, V // 2, 0, V - 1, 0, V // 3, -1])])
+    x = ref_rows(z, t, scale)
+    N = len(t)
+    zc, tc = z.cuda(), t.cuda()
+    r = tokens.logprobs(zc, tc, scale=scale, entropy=True)
+    g1, g2 = 64 * torch.randn(N, generator=g), 64 * torch.rand(N, generator=g)
+    for e in (None, g2):
+        d = tokens.logprobs_backward(zc, tc, r.lse, g1.cuda(), entropy=r.entropy, grad_entropy=None if e is None else e.cuda(), scale=scale)
+        want, size = ref_gradient(x, g1.double(), torch.zeros(N).double() if e is None else e.double(), scale)
+        # from the handed-over lse, rounded to fp32, as long as it is below 2^10; beyond from the row's own sums
+        lse = x["lse"].abs().nan_to_num(0, 0, 0)
+        close_gradient(d, want, size * (1 + torch.where(lse < 1024, lse, 0.0))[:, None], V, DT[dtype])
+        assert torch.isfinite(d).all()
+        own = torch.full((N, V + 1), 7.0, dtype=DT[dtype], device="cuda")
+        own[:, :V] = zc
+        again = tokens.logprobs_backward(own[:, :V], tc, r.lse, g1.cuda(), entropy=r.entropy, grad_entropy=None if e is None else e.cuda(), scale=scale, out=own[:, :V])
+        close_gradient(again, want, size * (1 + torch.where(lse < 1024, lse, 0.0))[:, None], V, DT[dtype])
+        assert (own[:, V] == 7).all()
