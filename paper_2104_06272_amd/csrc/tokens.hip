@@ -130,7 +130,8 @@ __device__ __forceinline__ void finish(const FinishArgs& a, FinishLds& lds)
     if (a.policy) {
         if (k == 0) m = W != 0.0 ? (v[1] + (a.kl != 0.0 ? a.kl * v[2] : 0.0) - (a.ent != 0.0 ? a.ent * v[3] : 0.0)) * inv : 0.0;
         if (k == 6) m = W;
-    } else {                                                            // loss, [h > 0], first, second, h, W, pairs, tokens
+    } else {                                                            // loss, [h > 0], first, second, h, W (broken pairs), pairs, tokens
+        if (k == 0 && v[5] != 0.0) m = (double)NAN;
         if (k == 5) m = W;
         if (k == 6) m = v[6];
     }
@@ -852,6 +853,7 @@ __global__ __launch_bounds__(1024) void pair_sums(const PairArgs a)
         const double h = a.beta * (D[0] - D[1]) - a.margin, y = a.label ? (double)a.label[k] : 1.0, w = a.weight ? (double)a.weight[k] : 1.0;
         if (a.margins && threadIdx.x == 0) a.margins[k] = (float)h;
         __syncthreads();                                                // (sums are read before the next pair's are written)
+        if (s[0].broken || s[1].broken) v[5] += 1.0;
         if (w == 0.0) continue;
         const double e = exp_of(-fabs(h)), up = reciprocal(1.0 + e), down = e * up;         // sigmoid(|h|), sigmoid(-|h|)
         const double soft = e < 1e-4 ? e * (1.0 - 0.5 * e) : log_of_sum(1.0 + e);                   // ln(1 + e^-|h|)

@@ -879,3 +879,15 @@ def test_backward_pass_of_masks_and_extremes(dtype, V, scale):
         again = tokens.logprobs_backward(own[:, :V], tc, r.lse, g1.cuda(), entropy=r.entropy, grad_entropy=None if e is None else e.cuda(), scale=scale, out=own[:, :V])
         close_gradient(again, want, size * (1 + torch.where(lse < 1024, lse, 0.0))[:, None], V, DT[dtype])
         assert (own[:, V] == 7).all()
+
+
+@gpu
+def test_a_broken_pair_without_weight_is_reported():
+    z, _, g = make_logits(50, 40, "fp32")
+    t = make_target(50, 40, g)
+    for seq in (tokens.packed(torch.tensor([0, 5, 3, 8, 50], device="cuda")), tokens.batch_major(4, 12, torch.tensor([12, 13, 3, 4], dtype=torch.int32, device="cuda")),
+                tokens.time_major(4, 12, torch.tensor([12, 12, 3, -1], dtype=torch.int32, device="cuda"))):
+        n = 50 if seq.offsets is not None else 48
+        for w in ([1.0, 0.0], [0.0, 0.0]):
+            q = tokens.preference_loss(z[:n], t[:n], seq, weight=torch.tensor(w, device="cuda"))
+            assert torch.isnan(q.loss), (seq.layout, w)
