@@ -3,7 +3,9 @@ policy loss, a loss over pairs of sequences, and lambda-returns over sequences o
 
 Argument marshalling only, like `binding`: PyTorch allocates outputs and workspace and provides the stream, all
 arithmetic runs in libanakin's kernels, there is no fallback.  Everything runs on the current stream of the tensors'
-device; nothing synchronises.  No gradients are recorded: a loss and its gradient towards the logits come from one call.
+device; nothing synchronises.  No gradients are recorded: a loss and its gradient towards the logits come from one call, and
+all inputs but the logits are constants to it.  Logits that autograd follows would lose that history without a word, so they are
+refused unless it is switched off (torch.no_grad): call with logits.detach() and hand the result to logits.backward(r.dlogits).
 
     logits      [rows][vocab], fp32, bf16 or fp16, columns adjacent, any distance from row to row
     target      [rows], uint8, int32 or int64: the chosen column; a row with a target outside [0, vocab) takes no part
@@ -85,9 +87,11 @@ def _refuse(why):
 class _Call:
     """The device and stream of one call, checks of its tensors, and the library's answer."""
 
-    def __init__(self, first):
+    def __init__(self, first, recorded=False):
         if not isinstance(first, torch.Tensor):
             _refuse("a tensor is wanted")
+        if recorded and first.requires_grad and torch.is_grad_enabled():
+            _refuse("no history is recorded: pass logits.detach() and hand dlogits to logits.backward")
         if not first.is_cuda:
             raise RuntimeError("the operators of token policies run on the GPU alone")
         self.L = binding.load()
@@ -122,6 +126,10 @@ class _Call:
             out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
         elif out.device != self.device or out.dtype != logits.dtype or out.shape != logits.shape or (out.shape[1] > 1 and out.stride(1) != 1):
             _refuse("out has to be like the logits: shape, type, device, adjacent columns")
+        elif out.requires_grad and torch.is_grad_enabled():
+            _refuse("out is written without history: pass out.detach()")
+        elif not out.is_inference():
+            torch.autograd.graph.increment_version(out)               # autograd's own copies of it are stale from here on
         return out, (out.stride(0) if out.shape[0] > 1 else out.shape[1])
 
     def sequences(self, q):
@@ -148,7 +156,7 @@ class _Call:
 def logprobs(logits, target, scale=1.0, entropy=False):
     """(logp, lse, entropy or None), fp32 [rows]: log-probability of the target under softmax(scale * logits), log-sum-exp,
     entropy.  Rows that take no part get zeros."""
-    c = _Call(logits)
+    c = _Call(logits, recorded=True)
     x = c.rows(logits, target, scale)
     logp, lse = c.empty(x.rows), c.empty(x.rows)
     h = c.empty(x.rows) if entropy else None
@@ -174,7 +182,7 @@ def policy_loss(logits, target, logp_old, adv, *, clip=0.2, kl_coef=0.0, logp_re
     r = exp(logp - logp_old), d = logp_ref - logp; the weighted mean over the rows that take part, and grad_scale times its
     gradient towards the logits.  clip: one width or (low, high).  norm: divide by this in place of the sum of the weights.
     gradient=False: the loss alone.  out: where the gradient goes (may be the logits themselves)."""
-    c = _Call(logits)
+    c = _Call(logits, recorded=True)
     x = c.rows(logits, target, scale)
     n = x.rows
     low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
@@ -194,7 +202,7 @@ def preference_loss(logits, target, sequences, *, beta=0.1, margin=0.0, mean=Fal
     log sigmoid(-h), h = beta (D_first - D_second) - margin, D the sum (mean: the mean) over a sequence's tokens of
     logp - logp_ref, y = label (None: 1, the first is the preferred one); the weighted mean over the pairs, and grad_scale
     times its gradient towards the logits.  margins: h of every pair."""
-    c = _Call(logits)
+    c = _Call(logits, recorded=True)
     x = c.rows(logits, target, scale)
     q = c.sequences(sequences)
     n, pairs = x.rows, q.count // 2

@@ -891,3 +891,38 @@ def test_a_broken_pair_without_weight_is_reported():
         for w in ([1.0, 0.0], [0.0, 0.0]):
             q = tokens.preference_loss(z[:n], t[:n], seq, weight=torch.tensor(w, device="cuda"))
             assert torch.isnan(q.loss), (seq.layout, w)
+
+
+def test_logits_that_record_gradients_are_refused():
+    z = torch.zeros(3, 5, requires_grad=True)
+    t, f = torch.zeros(3, dtype=torch.int64), torch.zeros(3)
+    for call in (lambda x: tokens.logprobs(x, t), lambda x: tokens.policy_loss(x, t, f, f), lambda x: tokens.preference_loss(x, t, tokens.batch_major(1, 3))):
+        for x in (z, z * 2):
+            with pytest.raises(binding.AnakinError, match="detach"):
+                call(x)
+        for x in (z.detach(), z):                                  # (these get as far as the device)
+            with torch.no_grad(), pytest.raises(RuntimeError, match="GPU"):
+                call(x)
+
+
+@gpu
+def test_gradients_in_place_are_seen_by_autograd():
+    leaf = torch.randn(4, 7, device="cuda", requires_grad=True)
+    t, f = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    lse = tokens.logprobs(leaf.detach(), t).lse
+    for call in (lambda z: tokens.policy_loss(z, t, f, f, out=z), lambda z: tokens.preference_loss(z, t, tokens.batch_major(2, 2), out=z), lambda z: tokens.logprobs_backward(z, t, lse, f, out=z)):
+        logits = leaf * 1.0
+        other = logits.square().sum()                              # keeps the logits for its backward pass
+        call(logits.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            other.backward()
+        with pytest.raises(binding.AnakinError):                   # an `out` whose history would be lost
+            tokens.policy_loss(logits.detach(), t, f, f, out=torch.zeros(4, 7, device="cuda", requires_grad=True))
+    # the pattern that the documentation names
+    logits = leaf * 1.0
+    r = tokens.policy_loss(logits.detach(), t, f, f + 1.0)
+    logits.backward(r.dlogits)
+    assert torch.equal(leaf.grad, r.dlogits)
+    with torch.inference_mode():
+        z = torch.randn(4, 7, device="cuda")
+        tokens.policy_loss(z, t, f, f, out=z)
