@@ -926,3 +926,93 @@ def test_gradients_in_place_are_seen_by_autograd():
     with torch.inference_mode():
         z = torch.randn(4, 7, device="cuda")
         tokens.policy_loss(z, t, f, f, out=z)
+
+
+# ---- accuracy: bounds that the arithmetic kept for it can hold, and no other ----------------------------------------------
+# The exponential instruction is good to one step, 2^-23 of its value; a quarter of that is allowed it as a mean over many rows.
+EXP_MEAN = 2.0 ** -25
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [4, 32, 64, 512, 1024, 4096, 32768])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.25])
+def test_pairs_do_not_see_a_number_added_to_a_row(dtype, V, scale):
+    """Logits on a grid, and the same with 4 more in every column: their distances to the maximum are the same numbers, so are the
+    log-probabilities, to the last bit (with the exponents' own roundings lost they would differ by some 1e-8 a row), and h is 0."""
+    n = 24
+    g = torch.Generator().manual_seed(V)
+    z = torch.randint(-12, 13, (n, V), generator=g) / 8.0         # up to 5.5 on steps of 1/8: 6 bits, which every type has
+    t = torch.randint(0, V, (n,), generator=g)
+    both = torch.cat([z, z + 4.0]).to(DT[dtype]).cuda()
+    assert torch.equal(both[:n].cpu().double() + 4.0, both[n:].cpu().double())
+    q = tokens.preference_loss(both, torch.cat([t, t]).cuda(), tokens.batch_major(2, n), beta=1.0, scale=scale)
+    assert float(q.margins[0]) == 0.0 and torch.equal(q.logp[:n], q.logp[n:])
+    assert torch.equal(q.dlogits[:n] == 0, q.dlogits[n:] == 0) and q.dlogits.any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V,n", [(3, 40000), (64, 20000), (1000, 8000), (8000, 1500), (40000, 400)])
+@pytest.mark.parametrize("scale", [0.7, 1.25, 0.79])
+def test_log_probabilities_have_no_drift(dtype, V, n, scale):
+    """Means over many rows, where roundings average out.  What is left is the exponential's own, n EXP_MEAN, and 6 times the root of
+    n roundings: for a sum of a pair's rows one of 2^-24 each, for outputs in fp32 one of U |logp|.  (scale log2 e rounded to fp32 is
+    off by up to 2^-24 of itself, at 0.79 by 5e-8: a mean logit of 25 turns that into 30 times EXP_MEAN if it is not put back.)"""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = (torch.randn(n, V, generator=g, device="cuda") * 2.5 + 24.0).to(DT[dtype])
+    t = torch.randint(0, V, (n,), generator=g, device="cuda")
+    lp = torch.empty(n, dtype=torch.float64)
+    for i in range(0, n, 2000):
+        x = z[i:i + 2000].cpu().double() * scale
+        m = x.max(1, keepdim=True).values
+        lp[i:i + 2000] = (x.gather(1, t[i:i + 2000].cpu()[:, None]) - m - torch.log(torch.exp(x - m).sum(1, keepdim=True)))[:, 0]
+    r = tokens.logprobs(z, t, scale=scale)
+    off = float((r.logp.cpu().double() - lp).mean())
+    assert abs(off) <= EXP_MEAN + 6 * U * float(lp.abs().max()) / math.sqrt(n), off
+    # (the margin takes h to 0, so that fp32 holds what is off)
+    q = tokens.preference_loss(z, t, tokens.packed(torch.tensor([0, n, n], device="cuda")), beta=1.0, margin=float(lp.sum()), scale=scale, gradient=False)
+    assert abs(float(q.margins[0])) <= n * EXP_MEAN + 6 * math.sqrt(n) * U, float(q.margins[0])
+
+
+@gpu
+@pytest.mark.parametrize("V,n", [(32768, 96), (131072, 64), (200003, 32)])
+def test_long_rows_add_up(V, n):
+    """Rows shifted to a log-sum-exp near 0, where fp32 holds it to 2^-30: root of the mean square of what it is off.  EXP_MEAN, and as
+    much for sums: a thread's chain of up to 64 additions, 2^-24 sqrt(64) / 2, over 256 threads at least, and their joins."""
+    g = torch.Generator().manual_seed(V)
+    z = torch.randn(n, V, generator=g) * 2.5
+    z = z - torch.logsumexp(z.double(), 1).float()[:, None] + torch.rand(n, 1, generator=g) * 0.02 - 0.01
+    t = torch.zeros(n, dtype=torch.int64)
+    off = tokens.logprobs(z.cuda(), t.cuda()).lse.cpu().double() - torch.logsumexp(z.double(), 1)
+    assert float((off ** 2).mean().sqrt()) <= 2 * EXP_MEAN
+
+
+@gpu
+def test_ratios_are_rounded_once():
+    """One column: the log-probability is 0, and the ratio e^-old rounded to fp32."""
+    z, t, one = torch.zeros(1, 1, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda"), torch.ones(1, device="cuda")
+    for i in range(60):
+        old = torch.tensor([1.0 - 0.21 * i])
+        r = tokens.policy_loss(z, t, old.cuda(), one, clip=(1.0, 1e6), gradient=False)
+        want = math.exp(-float(old[0]))
+        assert abs(float(r.stats[5]) - want) <= (U + 2.0 ** -36) * want and abs(float(r.loss) + want) <= (U + 2.0 ** -36) * want
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["packed", "batch", "time"])
+def test_share_of_pairs_the_first_wins(layout):
+    """The weighted share of pairs with h > 0, where no h is near 0 nor a sequence empty."""
+    pairs, n, V = 500, 3, 40
+    z, _, g = make_logits(2 * pairs * n, V, "fp32", seed=11)
+    t = make_target(2 * pairs * n, V, g)
+    seq = tokens.packed(torch.arange(0, 2 * pairs * n + 1, n, device="cuda")) if layout == "packed" else (tokens.batch_major if layout == "batch" else tokens.time_major)(2 * pairs, n)
+    rows = rows_of(layout, 2 * pairs, n, [n] * (2 * pairs))
+    weight = torch.rand(pairs, generator=g)
+    stats, h, _, _ = ref_preference(ref_rows(z, t, 1.0), rows, 0.5, 0.3, False, None, None, weight, 0.0)
+    near = np.abs(h) < 1e-4
+    weight[torch.tensor(near)] = 0.0
+    assert near.sum() < 5
+    want = float((weight.double().numpy() * (h > 0)).sum() / weight.double().sum())
+    q = tokens.preference_loss(z, t, seq, beta=0.5, margin=0.3, weight=weight.cuda())
+    assert abs(float(q.stats[1]) - want) <= 1.01 * U * want and 0.2 < want < 0.8
