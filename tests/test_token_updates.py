@@ -278,3 +278,158 @@ def test_metrics_are_those_of_the_update_made():
     g.set_policy_gradient(binding.PG_SCORE_FUNCTION)
     assert g.metrics() == want
     g.close()
+
+
+CHUNKED = [_cfg("catch_small"), _cfg("catch_4096", B=256, T=8), _cfg("catch_4096", hidden=[256], B=64, T=8), _cfg("maze_16384", hidden=[128, 128], B=64, T=8), _cfg("maze_16384", hidden=[256, 256], B=64, T=8)]
+
+
+@gpu
+@pytest.mark.parametrize("updates", [2, 4])
+@pytest.mark.parametrize("cfg", CHUNKED, ids=lambda c: f"{c['name']}-{'-'.join(map(str, c['net']['hidden']))}-{c['net']['dtype']}")
+def test_clipped_chunks_at_the_acting_parameters_are_the_score_functions(cfg, updates):
+    """Several updates whose gradients are all taken at the acting parameters: every chunk's ratio is 1."""
+    a, b = binding.Anakin(cfg, seed=2), binding.Anakin(cfg, seed=2)
+    for _ in range(6):
+        a.step(); b.step()
+    for g in (a, b):
+        g.set_updates_per_unroll(updates, sequential=False)
+    b.set_policy_gradient(binding.PG_CLIPPED)
+    b.set_clip(0.1, 0.3, 0.5)
+    tol = 2e-2 if cfg["net"]["dtype"] == "bf16" else 1e-4
+    start = a.get_params()
+    b.set_params(start)
+    b.set_opt_state(*a.get_opt_state())
+    a.rollout(); b.rollout()
+    a.learn(); b.learn()
+    regions, _ = PT.param_regions(cfg)
+    PT.assert_regions_close("gradient", b.get_grads(), a.get_grads(), regions, tol)
+    # (a step is the moments' ratio, to which the gradient adds a tenth: it is off by less than the gradient, in every update)
+    assert PT.rel(b.get_params() - start, a.get_params() - start) <= updates * tol
+    ma, mb, adv = a.metrics(), b.metrics(), b.trajectory()["adv"].astype(np.float64)
+    assert abs(mb["policy_loss"] + adv.mean()) <= 1e-5 * np.abs(adv).mean()
+    for k in ("value_loss", "entropy_loss"):
+        assert abs(mb[k] - ma[k]) <= 1e-5 * abs(ma[k]) + 1e-9, k
+    assert mb["reward_sum"] == ma["reward_sum"] and mb["episodes"] == ma["episodes"]
+    a.close(); b.close()
+
+
+@gpu
+@pytest.mark.parametrize("updates", [2, 4])
+@pytest.mark.parametrize("given", [False, True])
+def test_preference_chunks_at_the_acting_parameters(updates, given):
+    """Every chunk's gradient at the acting parameters, its own labels and weights; metrics are the chunks' means."""
+    B, T = 64, 20
+    cfg = _cfg("catch_small", hidden=[64, 64], B=B, T=T, lr=0.01)
+    g, theta0, (m, v, t) = _warm(cfg, seed=7)
+    g.set_policy_gradient(binding.PG_PREFERENCE)
+    gen = torch.Generator().manual_seed(1)
+    label, weight = torch.rand(updates, B // 2, generator=gen), torch.rand(updates, B // 2, generator=gen) * (torch.arange(B // 2) % 4 != 2)
+    g.set_preference(0.4, label.cuda(), weight.cuda()) if given else g.set_preference(0.4)
+    g.set_updates_per_unroll(updates, sequential=False)
+    g.learn()
+    tr, net = g.trajectory(), {k: float(np.float32(x)) for k, x in cfg["net"].items() if isinstance(x, float)}
+    x, act = torch.tensor(PT.np_observation(cfg, tr)), torch.tensor(tr["action"].astype(np.int64).ravel())
+    ret, rew = (torch.tensor(tr[k].astype(np.float64).ravel()) for k in ("ret", "reward"))
+    theta, m, v, n, losses = theta0.astype(np.float64), m.astype(np.float64), v.astype(np.float64), T // updates * B, []
+    for k in range(updates):
+        s = slice(k * n, (k + 1) * n)
+        th = torch.tensor(theta0.astype(np.float64)).requires_grad_(True)
+        head = _forward(cfg, th, x[s])
+        lp = torch.log_softmax(head[:, :-1], 1).gather(1, act[s, None]).reshape(-1)
+        d = (lp - lp.detach()).view(-1, B).sum(0)
+        h = 0.4 * (d[:B // 2] - d[B // 2:])
+        r = rew[s].view(-1, B).sum(0)
+        y = label[k].double() if given else 0.5 + 0.5 * torch.sign(r[:B // 2] - r[B // 2:])
+        w = weight[k].double() if given else torch.ones(B // 2).double()
+        policy = (w * -(y * torch.nn.functional.logsigmoid(h) + (1 - y) * torch.nn.functional.logsigmoid(-h))).sum() / w.sum()
+        value = net["value_coef"] * ((ret[s] - head[:, -1]) ** 2).mean()
+        (policy + value).backward()
+        grad = th.grad.numpy()
+        t += 1
+        m, v = net["beta1"] * m + (1 - net["beta1"]) * grad, net["beta2"] * v + (1 - net["beta2"]) * grad * grad
+        theta = theta - net["lr"] * (m / (1 - net["beta1"] ** t)) / (np.sqrt(v / (1 - net["beta2"] ** t)) + net["eps"])
+        losses.append([float(policy.detach()), float(value.detach())])
+    PT.assert_regions_close("gradient", g.get_grads(), grad, PT.param_regions(cfg)[0], 1e-4)
+    assert PT.rel(g.get_params() - theta0, theta - theta0) <= updates * 1e-4
+    got, want = g.metrics(), np.array(losses).mean(0)
+    assert abs(got["policy_loss"] - want[0]) <= 1e-5 * want[0] and abs(got["value_loss"] - want[1]) <= 1e-4 * want[1] and got["entropy_loss"] == 0.0
+    g.close()
+
+
+def _maze_gradient(cfg, theta, walls, pos, acts, loss_of):
+    """The gradient of loss_of(head outputs) in binary64 from stored bf16 activations acts[l] [T][B][H]; weights as the forward pass saw
+    them."""
+    hid, cells, off, Ws = list(cfg["net"]["hidden"]), walls.shape[1], 0, []
+    th = theta.astype(np.float32)
+    for k, n in zip([3 * cells] + hid, hid):
+        Ws.append(PT.bf16_round_np(th[off:off + k * n]).astype(np.float64).reshape(k, n)); off += k * n + n
+    A = 4
+    Wh = PT.bf16_round_np(th[off:off + hid[-1] * (A + 1)]).astype(np.float64).reshape(hid[-1], A + 1)
+    bh = th[off + hid[-1] * (A + 1):].astype(np.float64)
+    h = [a.reshape(-1, a.shape[-1]).astype(np.float64) for a in acts]
+    head = torch.tensor(h[-1] @ Wh + bh, requires_grad=True)
+    loss_of(head).backward()
+    d = head.grad.numpy()
+    tail = [(h[-1].T @ d).ravel(), d.sum(0)]
+    dz = (h[-1] > 0) * (d @ Wh.T)
+    for l in range(len(hid) - 1, 0, -1):
+        tail = [(h[l - 1].T @ dz).ravel(), dz.sum(0)] + tail
+        dz = (h[l - 1] > 0) * (dz @ Ws[l].T)
+    M = len(dz)
+    x = np.zeros((M, 3 * cells))
+    x[:, :cells] = np.tile(walls, (M // len(walls), 1))
+    x[np.arange(M), cells + pos.reshape(-1)] = 1.0
+    x[:, -1] = 1.0
+    return np.concatenate([(x.T @ dz).ravel(), dz.sum(0)] + tail)
+
+
+@gpu
+@pytest.mark.parametrize("updates", [2, 4])
+@pytest.mark.parametrize("kind", [binding.PG_CLIPPED, binding.PG_PREFERENCE])
+@pytest.mark.parametrize("hidden", [[128, 128], [256, 256]])
+def test_sequential_bf16_updates(hidden, kind, updates):
+    """The last chunk of a bf16 maze net: its gradient at the parameters that the chunks before left (the last step taken back from the
+    moments), its ratios against the head outputs stored at acting time."""
+    B, T = 64, 8
+    cfg = _cfg("maze_16384", hidden=hidden, B=B, T=T, lr=0.003)
+    g, _, _ = _warm(cfg, seed=5)
+    g.set_policy_gradient(kind)
+    g.set_clip(0.02, 0.03, 0.2)
+    g.set_preference(0.4)
+    g.set_updates_per_unroll(updates, sequential=True)
+    old = g.trajectory()["head"][:T].astype(np.float64)
+    g.learn()
+    tr, net = g.trajectory(), {k: float(np.float32(v)) for k, v in cfg["net"].items() if isinstance(v, float)}
+    m, v, t = g.get_opt_state()
+    step = net["lr"] * (m / (1 - net["beta1"] ** t)) / (np.sqrt(v.astype(np.float64) / (1 - net["beta2"] ** t)) + net["eps"])
+    theta = (g.get_params() + step).astype(np.float32)
+    walls = np.unpackbits(g.get_walls().view(np.uint8), axis=1, bitorder="little")[:, :256].astype(bool)
+    s = slice(T - T // updates, T)
+    pos, acts = (tr["state_s0"][s] & 0xffff).astype(np.int64), [a[s] for a in tr["act"]]
+    # the forward pass was repeated there: every layer from the one before
+    for _, _, refs, _ in PT.np_maze_forward_layers_from_stored(cfg, theta, walls, pos, acts, t_chunk=T):
+        for l, r in enumerate(refs):
+            PT.assert_bf16_layers_close(f"layer {l + 1}", acts[l], r)
+    act = torch.tensor(tr["action"][s].astype(np.int64).ravel())[:, None]
+    adv, ret = (torch.tensor(tr[k][s].astype(np.float64).ravel()) for k in ("adv", "ret"))
+    lp_old = torch.log_softmax(torch.tensor(old[s].reshape(-1, 5)[:, :4]), 1).gather(1, act).reshape(-1)
+    share = []
+
+    def loss_of(head):
+        logs = torch.log_softmax(head[:, :4], 1)
+        lp = logs.gather(1, act).reshape(-1)
+        value = net["value_coef"] * ((ret - head[:, 4]) ** 2).mean()
+        if kind == binding.PG_CLIPPED:
+            r, d = torch.exp(lp - lp_old), lp_old - lp
+            share.append(float((r * adv > r.clamp(0.98, 1.03) * adv).double().mean()))
+            return (-torch.minimum(r * adv, r.clamp(0.98, 1.03) * adv) + 0.2 * (torch.exp(d) - d - 1)).mean() + net["entropy_coef"] * (torch.exp(logs) * logs).sum(1).mean() + value
+        D = (lp - lp_old).view(-1, B).sum(0)
+        h = 0.4 * (D[:B // 2] - D[B // 2:])
+        share.append(float((h.abs() > 1e-3).double().mean()))
+        rew = torch.tensor(tr["reward"][s].astype(np.float64)).sum(0)
+        y = 0.5 + 0.5 * torch.sign(rew[:B // 2] - rew[B // 2:])
+        return -(y * torch.nn.functional.logsigmoid(h) + (1 - y) * torch.nn.functional.logsigmoid(-h)).mean() + value
+    want = _maze_gradient(cfg, theta, walls, pos, acts, loss_of)
+    PT.assert_regions_close("gradient", g.get_grads(), want, PT.param_regions(cfg)[0], 2e-2)
+    assert share[0] > 0.02                                        # the policy has moved
+    g.close()
