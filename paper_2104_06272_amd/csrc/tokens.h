@@ -127,8 +127,11 @@ __device__ __forceinline__ Shift shift_of(float m, float c)
 
 // Sums over part of a row: s = sum 2^t, and beside it either u = sum t 2^t (the entropy) or, `fine`, u = sum r 2^t with r what
 // rounding took from the exponents: there t = fl(c x), x = z - m, and r = c x - t with c to 48 bits.  r matters where thousands
-// of log-probabilities are summed and two such sums subtracted.  Elements of minus infinity add 0 (their t or r enters u
-// clamped); a NaN stays in s.
+// of log-probabilities are summed and two such sums subtracted.  Of 16-bit logits x is exact and r is all that was lost; of fp32
+// logits x is rounded itself, which r does not hold (root mean square of what a log-sum of 3 to 1024 columns around 0 is off by,
+// exponentials rounded to nearest: coarse 5 to 23e-9; fine 2 to 7e-9 with 16 bits, 3 to 9e-9 with fp32).  A number added to all of
+// a row, where the type holds the sums, changes nothing.  Elements of minus infinity add 0 (their t or r enters u clamped); a NaN
+// stays in s.
 struct Part { float m, s, u; };
 // what t changes by from one maximum to a larger one
 __device__ __forceinline__ float step_between(float from, float to, float c)

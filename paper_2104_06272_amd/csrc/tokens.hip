@@ -1011,7 +1011,10 @@ static hipError_t launch_sums(int type, const SumArgs& a, bool fine, hipStream_t
         else BY_TYPE(type, launch_lanes, DO_SUMS, false)(f, l, lane_grid(f, a.r.rows), s);
     } else {
         // Fewer rows than compute units: 16 pieces a thread (one row of 131072 bf16 with 256 threads 11.7 us, with 1024 10.2; 64 x 8192
-        // 4.1 and 5.0).  Many rows: the shorter they are the fewer threads, so that more of them are on their way.
+        // 4.1 and 5.0).  Many rows: the shorter they are the fewer threads, so that more of them are on their way.  At the borders, bf16
+        // from the caches, us with 128, 256, 512 and 1024 threads: 256 x 131072 25.3, 17.0, 15.9, 17.3 and 257 34.5, 20.5, 21.0, 24.3;
+        // 256 x 32768 8.5, 6.5, 6.1, 6.4 and 257 10.8, 7.9, 7.4, 10.3; 512 x 131072 36.2, 23.9, 28.0, 31.6 and 513 36.1, 29.2, 29.8, 35.3;
+        // 512 x 32768 11.6, 8.4, 8.1, 10.9; 512 x 8192 5.7, 5.0, 5.9, 7.6 and (64 threads 6.1) 513 5.7, 5.2, 6.5, 9.8.
         const int64_t pieces = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8);
         const int few = pieces >= 12288 ? 1024 : pieces >= 6144 ? 512 : 256, many = pieces <= 1024 ? 64 : pieces <= 2048 ? 128 : 256;
         const dim3 grid((unsigned)a.r.rows), block(a.r.rows <= 256 ? few : a.r.rows <= 512 ? 256 : many);
@@ -1037,7 +1040,9 @@ static hipError_t launch_gradients(int type, const GradArgs& a, bool ent, hipStr
         const bool brief = a.r.V / (type == ANAKIN_TYPE_FP32 ? 4 : 8) <= 1024;
         auto k = brief ? (ent ? BY_TYPE(type, block_gradients, true, false, 64) : a.ws ? BY_TYPE(type, block_gradients, false, true, 64) : BY_TYPE(type, block_gradients, false, false, 64))
                        : (ent ? BY_TYPE(type, block_gradients, true, false, WG) : a.ws ? BY_TYPE(type, block_gradients, false, true, WG) : BY_TYPE(type, block_gradients, false, false, WG));
-        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 3.5 us)
+        // few rows: shares of them, until there are four workgroups to a compute unit (one row of 131072 bf16 10.3 -> 3.5 us; us with 1,
+        // 2, 4 and 8 shares: 16 rows 10.5, 7.0, 5.1, 4.2; 64 12.2, 9.3, 7.5, 7.1; 256 22.8, 22.5, 22.3, 22.2; 512 42.5, 42.0, 42.1, 41.4;
+        // 1500 153, 152, 150, 144)
         GradArgs b = a;
         const int64_t rounds = a.r.V / ((type == ANAKIN_TYPE_FP32 ? 4 : 8) * loads_in_flight(WG) * WG);
         b.shares = brief || a.r.rows >= 1024 || rounds < 2 ? 1 : (int)(1024 / (a.r.rows > 0 ? a.r.rows : 1) < rounds ? 1024 / (a.r.rows > 0 ? a.r.rows : 1) : rounds);
